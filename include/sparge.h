@@ -284,6 +284,95 @@ int sparge_permute_tokens(const void* src, const sparge_desc* desc, const int32_
                           int offset, int inverse, void* dst, void* hip_stream);
 
 /*
+ * Paged 8-bit K/V cache: what a program that answers token by token keeps of the tokens it has attended, and the attention
+ * of new tokens over it.  One sparge_cache serves one attention layer's R rows (requests); programs of several layers
+ * share the bookkeeping (table, length, free_pages, n_free) between layers' structs and plan once per step.
+ *
+ * Pages hold SPARGE_CACHE_PAGE = 64 tokens; block b of row r (tokens [64 b, 64 b + 64)) lies in page table[r, b].  Per page
+ * and kv head, K and V are stored as 8-bit codes with one scale each: amax = max |x| over the block's tokens so far,
+ * code = 127 x / amax rounded to nearest, ties to even, of the exact quotient; the value it stands for is code amax / 127.
+ * For K, x = fp32(K) - k_shift[r] where a shift is given (any vector per row and kv head, such as sparge_quantize's k_mean
+ * of the prompt: softmax is invariant to it; it must not change while the row holds tokens).  A block with a NaN or an
+ * infinity has codes 0 and that amax: every query that sees a key of the block gets NaN.
+ * The tokens of a row's open (last, partial) block are kept in 16 bits in k_tail / v_tail as well, so that its codes always
+ * come from the tokens themselves: however a row's tokens were appended, its codes and scales are the same bits.
+ *
+ * All pointers are device memory of the caller: k, v, k_tail, v_tail, k_shift 16-byte aligned, the others 4.  k, v: bytes
+ * [n_pages, H_kv, 64 d] in an order of the library's own (sparge_cache_read gives tokens).  To start: length all 0,
+ * free_pages the page numbers 0..n_pages-1 in any order (taken from the end), *n_free = n_pages; nothing else needs a value.
+ * The entry points allocate nothing, never synchronise and take everything that changes from step to step from device
+ * memory, so that a step can be captured into a graph once and replayed.  Row counts, slots and page numbers found in
+ * device memory are checked by the kernels: what lies outside the arrays is skipped, never read or written.
+ * Limits: d in {64, 128}, fp16 or bf16, R <= SPARGE_CACHE_MAX_ROWS, n_pages and max_blocks <= 2^24.
+ */
+enum { SPARGE_F32 = 2 /* sparge_cache_read's output only */ };
+enum { SPARGE_CACHE_PAGE = 64, SPARGE_CACHE_MAX_ROWS = 4096 };
+/* bits of sparge_cache_plan's status[0] */
+enum { SPARGE_CACHE_NO_PAGES = 1, SPARGE_CACHE_ROW_FULL = 2, SPARGE_CACHE_NO_SLOTS = 4, SPARGE_CACHE_BAD_STATE = 8 };
+
+typedef struct sparge_cache {
+    int32_t R, H_kv, d, dtype;          /* dtype: of the tokens (and of Q and O), SPARGE_F16 | SPARGE_BF16 */
+    int32_t n_pages, max_blocks;
+    void *k, *v;                        /* [n_pages, H_kv, 64 d] bytes */
+    float *k_amax, *v_amax;             /* [n_pages, H_kv] */
+    void *k_tail, *v_tail;              /* 16-bit [R, H_kv, 64, d] */
+    int32_t* table;                     /* [R, max_blocks] */
+    int32_t* length;                    /* [R] tokens that row r holds */
+    int32_t* free_pages;                /* [n_pages] stack of free pages */
+    int32_t* n_free;                    /* [1] */
+    const float* k_shift;               /* [R, H_kv, d] or NULL */
+} sparge_cache;
+
+/*
+ * The bookkeeping of one step.  Rows with release[r] != 0 (release may be NULL: none) give up their pages, pushed onto the
+ * free stack by ascending row and block, and are empty; then every row takes the pages that its new_len[r] >= 0 new tokens
+ * need from the top of the stack, by ascending row and block, and length[r] grows by new_len[r].
+ * Outputs: cu int32 [R + 1], prefix sums of new_len; for the new tokens i = cu[r] .. cu[r+1] - 1, the ones that the
+ * program's tensors hold in this order, slots[i] = 64 page + position % 64 and req[i] = r (int32 [n_slots]; -1 behind the
+ * last one); status int32 [2] = {0, free pages left}.  All or nothing: where the free pages, a row's max_blocks or n_slots do
+ * not suffice, or lengths or n_free are not ones that this call leaves, status[0] tells which (SPARGE_CACHE_* bits,
+ * BAD_STATE alone), nothing of the cache changes, cu is all 0 and slots and req all -1: the calls below then do nothing.
+ * n_slots may be 0 (slots, req NULL): a step that only releases.
+ */
+int sparge_cache_plan(const sparge_cache* cache, const int32_t* new_len, const uint8_t* release, int n_slots, int32_t* cu,
+                      int32_t* slots, int32_t* req, int32_t* status, void* hip_stream);
+
+/*
+ * Stores the step's new tokens: K, V 16-bit [n_slots, H_kv, d] (element strides per token and head, multiples of 8; d
+ * contiguous; 16-byte aligned), token i to slots[i] of row req[i], as sparge_cache_plan gave them.  Every page that gets
+ * a token is quantized anew from all its tokens.  Tokens with slot -1 are skipped.  The same call may be repeated as long as
+ * the step's tokens did not open another page of a row whose last page was partly filled.
+ */
+int sparge_cache_append(const sparge_cache* cache, const void* K, const void* V, int n_slots, int64_t k_stride_n,
+                        int64_t k_stride_h, int64_t v_stride_n, int64_t v_stride_h, const int32_t* cu, const int32_t* slots,
+                        const int32_t* req, void* hip_stream);
+
+/*
+ * Reads tokens back as the values that their codes stand for (with k_shift added again): K, V [n_slots, H_kv, d]
+ * contiguous, 16-byte aligned, SPARGE_F32 (code amax / 127 + shift rounded once) or the cache's dtype (that, rounded to it).
+ * slots: any, in any order (64 table[r, t / 64] + t % 64 for token t of row r); outputs of slots outside the pool stay as
+ * they were.  req: the rows, for k_shift (NULL allowed without).
+ */
+int sparge_cache_read(const sparge_cache* cache, const int32_t* slots, const int32_t* req, int n_slots, int out_dtype, void* K,
+                      void* V, void* hip_stream);
+
+/*
+ * Attention of the step's tokens over the cache, after sparge_cache_append: H query heads in groups of H / H_kv that share a
+ * kv head (head h reads kv head h / (H / H_kv)).  Q, O: 16-bit [n_slots, H, d] (strides as above).  Token i = cu[r] + t of row r
+ * sees the keys 0 .. p + t, p = length[r] - (cu[r+1] - cu[r]), or all of the row's keys if causal = 0; of these only
+ * blocks with mask[r, kv head, block] != 0 (uint8 [R, H_kv, max_blocks], NULL: all).
+ * O_i = sum_j softmax_j(sm_scale q_i . k_j) v_j over the keys that it sees, 0 if there are none; rows of O behind
+ * cu[R] stay as they were.  sm_scale <= 0 selects 1/sqrt(d).
+ * Products are 16-bit with fp32 sums; the codes enter them exactly (integers up to 127 in fp16), Q as it is (bf16 times a
+ * power of two per row, in fp16), the weights rounded to fp16.  The result does not depend on timing.
+ * The workspace (256-byte aligned) carries nothing between calls; calls that may overlap need one each.
+ */
+int sparge_cache_attn_workspace_bytes(const sparge_cache* cache, int H, size_t* bytes /* host, out */);
+int sparge_cache_attn(const sparge_cache* cache, const void* Q, int n_slots, int H, int64_t q_stride_n, int64_t q_stride_h,
+                      const int32_t* cu, const uint8_t* mask, float sm_scale, int causal, void* O, int64_t o_stride_n,
+                      int64_t o_stride_h, void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
  * Profiling aid (not part of the method).  Hands the library `n` pairs of caller-created hipEvent_t
  * (host arrays of handles).  From then on, every launch of the attention kernel made by the calling
  * thread is bracketed on its stream by hipEventRecord(starts[k]), hipEventRecord(stops[k]), k counting

@@ -31,6 +31,12 @@ class _Desc(ctypes.Structure):
                 ("stride_n", ctypes.c_int64), ("pv_dtype", ctypes.c_int32), ("qk_dtype", ctypes.c_int32)]
 
 
+class _Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("R", "H_kv", "d", "dtype", "n_pages", "max_blocks")] + [
+        (n, ctypes.c_void_p) for n in ("k", "v", "k_amax", "v_amax", "k_tail", "v_tail", "table", "length", "free_pages",
+                                       "n_free", "k_shift")]
+
+
 def library_path() -> str:
     """The in-tree library; SPARGE_LIBRARY overrides it (e.g. to load an experimental build)."""
     return os.environ.get("SPARGE_LIBRARY") or os.path.join(os.path.dirname(os.path.abspath(__file__)),
@@ -81,7 +87,15 @@ def load_library() -> ctypes.CDLL:
                                 ctypes.c_size_t, vp]
     lib.sparge_forward.argtypes = [vp, vp, vp, dp, f32p, f32p, f32p, ctypes.c_float, ctypes.c_int, vp, vp, vp, vp,
                                    ctypes.c_size_t, vp]
-    for name in ("sparge_workspace_bytes", "sparge_quantize", "sparge_predict", "sparge_attn_quantized",
+    cp, i64 = ctypes.POINTER(_Cache), ctypes.c_int64
+    lib.sparge_cache_plan.argtypes = [cp, vp, vp, ctypes.c_int, vp, vp, vp, vp, vp]
+    lib.sparge_cache_append.argtypes = [cp, vp, vp, ctypes.c_int, i64, i64, i64, i64, vp, vp, vp, vp]
+    lib.sparge_cache_read.argtypes = [cp, vp, vp, ctypes.c_int, ctypes.c_int, vp, vp, vp]
+    lib.sparge_cache_attn_workspace_bytes.argtypes = [cp, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]
+    lib.sparge_cache_attn.argtypes = [cp, vp, ctypes.c_int, ctypes.c_int, i64, i64, vp, vp, ctypes.c_float, ctypes.c_int, vp, i64,
+                                      i64, vp, ctypes.c_size_t, vp]
+    for name in ("sparge_cache_plan", "sparge_cache_append", "sparge_cache_read", "sparge_cache_attn_workspace_bytes",
+                 "sparge_cache_attn", "sparge_workspace_bytes", "sparge_quantize", "sparge_predict", "sparge_attn_quantized",
                  "sparge_attn", "sparge_forward", "sparge_mask_to_lut", "sparge_item_order", "sparge_v_tiles", "sparge_attn_tiled", "sparge_v_tiles_bytes",
                  "sparge_rel_l1", "sparge_tune_workspace_bytes", "sparge_tune_workspace_batched_bytes", "sparge_tune", "sparge_hilbert_order",
                  "sparge_permute_tokens"):
@@ -405,6 +419,171 @@ def sparge_permute_tokens(x: torch.Tensor, perm: torch.Tensor, offset: int = 0, 
     _check(load_library().sparge_permute_tokens(_ptr(x), ctypes.byref(d), _ptr(perm), perm.numel(), int(offset),
                                                 int(inverse), _ptr(y), _stream()))
     return y
+
+
+CACHE_PAGE = 64  # SPARGE_CACHE_PAGE
+CACHE_NO_PAGES, CACHE_ROW_FULL, CACHE_NO_SLOTS, CACHE_BAD_STATE = 1, 2, 4, 8  # bits of CachePlan.status[0]
+
+
+class SpargeCache:
+    """The tensors of one layer's paged 8-bit K/V cache (sparge.h, sparge_cache).  `book` holds what changes from step to step but
+    the pages (n_free, length [R], free_pages [n_pages], table [R, max_blocks], int32, one tensor): a copy of it is a point to
+    go back to.  share: a cache of the same rows and pages whose book this one uses, too (the layers of a model plan once
+    per step).  k_shift: fp32 [R, H_kv, d] or None; it must not change while rows hold tokens."""
+
+    def __init__(self, rows: int, kv_heads: int, head_dim: int, n_pages: int, max_blocks: int, dtype: torch.dtype = torch.bfloat16,
+                 device="cuda", k_shift: Optional[torch.Tensor] = None, share: Optional["SpargeCache"] = None):
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise SpargeError(f"dtype {dtype} not supported (fp16 or bf16)")
+        if min(rows, kv_heads, n_pages, max_blocks) < 1 or max(n_pages, max_blocks) > 1 << 24 or rows > 4096 or head_dim not in (64, 128):
+            raise SpargeError("rows, kv_heads, n_pages, max_blocks must be >= 1 (at most 4096 rows, 2^24 pages and blocks), head_dim 64 or 128")
+        self.rows, self.kv_heads, self.head_dim = rows, kv_heads, head_dim
+        self.n_pages, self.max_blocks, self.dtype = n_pages, max_blocks, dtype
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise SpargeError("the cache must live on the GPU")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        if share is not None:
+            if (share.rows, share.n_pages, share.max_blocks, share.device) != (rows, n_pages, max_blocks, self.device):
+                raise SpargeError("a shared book needs the same rows, pages, blocks and device")
+            self.book = share.book
+        else:
+            self.book = torch.zeros(1 + rows + n_pages + rows * max_blocks, dtype=torch.int32, device=self.device)
+        self.n_free, self.length = self.book[:1], self.book[1:1 + rows]
+        self.free_pages = self.book[1 + rows:1 + rows + n_pages]
+        self.table = self.book[1 + rows + n_pages:].view(rows, max_blocks)
+        if share is None:
+            self.n_free.fill_(n_pages)
+            self.free_pages.copy_(torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=self.device))  # page 0 goes first
+            self.table.fill_(-1)
+        empty = lambda *s, dt: torch.empty(s, dtype=dt, device=self.device)
+        self.k, self.v = (empty(n_pages, kv_heads, CACHE_PAGE * head_dim, dt=torch.uint8) for _ in range(2))
+        self.k_amax, self.v_amax = (torch.zeros((n_pages, kv_heads), dtype=torch.float32, device=self.device) for _ in range(2))
+        self.k_tail, self.v_tail = (empty(rows, kv_heads, CACHE_PAGE, head_dim, dt=dtype) for _ in range(2))
+        if k_shift is not None:
+            _array(k_shift, torch.float32, (rows, kv_heads, head_dim), self.device, "k_shift")
+        self.k_shift = k_shift
+        self._struct = _Cache(rows, kv_heads, head_dim, 0 if dtype == torch.float16 else 1, n_pages, max_blocks,
+                              *[None if t is None else t.data_ptr() for t in (
+                                  self.k, self.v, self.k_amax, self.v_amax, self.k_tail, self.v_tail, self.table, self.length,
+                                  self.free_pages, self.n_free, k_shift)])
+
+
+class CachePlan:
+    """What sparge_cache_plan gives: cu int32 [R + 1], slots and req int32 [n_slots], status int32 [2]."""
+
+    def __init__(self, cu: torch.Tensor, slots: torch.Tensor, req: torch.Tensor, status: torch.Tensor):
+        self.cu, self.slots, self.req, self.status = cu, slots, req, status
+
+
+def _array(t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], device: torch.device, name: str) -> None:
+    if tuple(t.shape) != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise SpargeError(f"{name} must be a contiguous {dtype} {list(shape)} tensor on {device}")
+
+
+def _tokens(t: torch.Tensor, cache: SpargeCache, n_slots: int, heads: Optional[int], name: str) -> None:
+    if t.dim() != 3 or t.shape[0] != n_slots or t.shape[2] != cache.head_dim or (heads is not None and t.shape[1] != heads):
+        raise SpargeError(f"{name} must be [{n_slots}, {'H' if heads is None else heads}, {cache.head_dim}], not {list(t.shape)}")
+    if t.dtype != cache.dtype or t.device != cache.device:
+        raise SpargeError(f"{name} must be {cache.dtype} on {cache.device}")
+    if t.stride(2) != 1 and t.numel():
+        raise SpargeError("the head dimension must be contiguous")
+
+
+def _on(cache: SpargeCache):
+    """The cache's device made current for a call (and the stream that is current there)."""
+    return torch.cuda.device(cache.device)
+
+
+def sparge_cache_plan(cache: SpargeCache, new_len: torch.Tensor, n_slots: int, release: Optional[torch.Tensor] = None,
+                      out: Optional[CachePlan] = None) -> CachePlan:
+    """One step's pages, block table and slot map.  new_len: int32 [R] on the GPU, tokens that each row adds; n_slots: rows of the
+    step's token tensors (at least the sum of new_len); release: uint8 [R], rows that give up what they hold first.  Where
+    it does not fit, plan.status[0] is not 0, nothing changes and the plan is empty (read it to find out: no call here waits)."""
+    _array(new_len, torch.int32, (cache.rows,), cache.device, "new_len")
+    if release is not None:
+        _array(release, torch.uint8, (cache.rows,), cache.device, "release")
+    if out is None:
+        new = lambda n: torch.empty(n, dtype=torch.int32, device=cache.device)
+        out = CachePlan(new(cache.rows + 1), new(n_slots), new(n_slots), new(2))
+    for name, t, n in (("cu", out.cu, cache.rows + 1), ("slots", out.slots, n_slots), ("req", out.req, n_slots), ("status", out.status, 2)):
+        _array(t, torch.int32, (n,), cache.device, f"plan.{name}")
+    with _on(cache):
+        _check(load_library().sparge_cache_plan(ctypes.byref(cache._struct), _ptr(new_len), _ptr(release), n_slots, _ptr(out.cu),
+                                                _ptr(out.slots), _ptr(out.req), _ptr(out.status), _stream()))
+    return out
+
+
+def sparge_cache_append(cache: SpargeCache, K: torch.Tensor, V: torch.Tensor, plan: CachePlan) -> None:
+    """Stores the step's tokens, K, V [n_slots, H_kv, d], where the plan says."""
+    n = plan.slots.numel()
+    _tokens(K, cache, n, cache.kv_heads, "K")
+    _tokens(V, cache, n, cache.kv_heads, "V")
+    _plan_arrays(cache, plan)
+    with _on(cache):
+        _check(load_library().sparge_cache_append(ctypes.byref(cache._struct), _ptr(K), _ptr(V), n, K.stride(0), K.stride(1),
+                                                  V.stride(0), V.stride(1), _ptr(plan.cu), _ptr(plan.slots), _ptr(plan.req), _stream()))
+
+
+def _plan_arrays(cache: SpargeCache, plan: CachePlan) -> None:
+    n = plan.slots.numel()
+    _array(plan.cu, torch.int32, (cache.rows + 1,), cache.device, "plan.cu")
+    _array(plan.slots, torch.int32, (n,), cache.device, "plan.slots")
+    _array(plan.req, torch.int32, (n,), cache.device, "plan.req")
+
+
+def sparge_cache_read(cache: SpargeCache, slots: torch.Tensor, req: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
+                      out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """-> K, V [n, H_kv, d]: the values that the codes of these slots (int32 [n]) stand for, in fp32 or the cache's dtype (default).
+    req: the slots' rows, int32 [n], for a cache with k_shift.  Outputs of slots outside the pool are left as they were."""
+    dtype = dtype or cache.dtype
+    if dtype not in (torch.float32, cache.dtype):
+        raise SpargeError(f"dtype {dtype} is neither fp32 nor the cache's {cache.dtype}")
+    if slots.dim() != 1:
+        raise SpargeError("slots must be a vector")
+    n = slots.numel()
+    _array(slots, torch.int32, (n,), cache.device, "slots")
+    if req is not None:
+        _array(req, torch.int32, (n,), cache.device, "req")
+    K, V = out if out is not None else (torch.empty((n, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.device) for _ in range(2))
+    _array(K, dtype, (n, cache.kv_heads, cache.head_dim), cache.device, "K")
+    _array(V, dtype, (n, cache.kv_heads, cache.head_dim), cache.device, "V")
+    code = 2 if dtype == torch.float32 else cache._struct.dtype
+    with _on(cache):
+        _check(load_library().sparge_cache_read(ctypes.byref(cache._struct), _ptr(slots), _ptr(req), n, code, _ptr(K), _ptr(V), _stream()))
+    return K, V
+
+
+def sparge_cache_attn_workspace_bytes(cache: SpargeCache, H: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().sparge_cache_attn_workspace_bytes(ctypes.byref(cache._struct), H, ctypes.byref(n)))
+    return int(n.value)
+
+
+def sparge_cache_attn(cache: SpargeCache, Q: torch.Tensor, plan: CachePlan, causal: bool = True, sm_scale: float = 0.0,
+                      mask: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the step's tokens, Q [n_slots, H, d], over the cache (after sparge_cache_append).  mask: uint8
+    [R, H_kv, max_blocks], 0 = no key of that block is seen.  -> O like Q (rows that are no token of the step: as they were)."""
+    n = plan.slots.numel()
+    _tokens(Q, cache, n, None, "Q")
+    _plan_arrays(cache, plan)
+    H = Q.shape[1]
+    if mask is not None:
+        _array(mask, torch.uint8, (cache.rows, cache.kv_heads, cache.max_blocks), cache.device, "mask")
+    O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device) if out is None else out
+    _tokens(O, cache, n, H, "out")
+    need = sparge_cache_attn_workspace_bytes(cache, H)
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
+    elif ws.device != cache.device or not ws.is_contiguous():
+        raise SpargeError(f"ws must be contiguous on {cache.device}")
+    with _on(cache):
+        _check(load_library().sparge_cache_attn(ctypes.byref(cache._struct), _ptr(Q), n, H, Q.stride(0), Q.stride(1), _ptr(plan.cu),
+                                                _ptr(mask), float(sm_scale), int(causal), _ptr(O), O.stride(0), O.stride(1),
+                                                _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    return O
 
 
 class AttnKernelTimer:

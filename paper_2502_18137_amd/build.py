@@ -26,6 +26,8 @@ SOURCES = {
     "v_fp8.hip": ["-ffp-contract=off"],
     "metrics.hip": ["-ffp-contract=off"],
     "permute.hip": [],
+    "cache.hip": ["-ffp-contract=off"],
+    "cache_attn.hip": [],
     "api.hip": [],
 }
 

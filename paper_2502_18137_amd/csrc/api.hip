@@ -12,6 +12,7 @@
 #include <mutex>
 #include <vector>
 
+#include "cache.hpp"
 #include "common.hpp"
 
 using namespace sparge;
@@ -100,6 +101,45 @@ const float* v_scale_of(const void* v_tiles, const Shape& s) {
 }
 
 bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+bool off4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+
+int check_cache(const sparge_cache* c, bool table) {
+    if (!c) return fail(SPARGE_EINVAL, "cache is NULL");
+    if (c->R < 1 || c->H_kv < 1 || c->n_pages < 1 || c->max_blocks < 1)
+        return fail(SPARGE_EINVAL, "R, H_kv, n_pages, max_blocks must be >= 1 (got %d, %d, %d, %d)", c->R, c->H_kv, c->n_pages, c->max_blocks);
+    if (c->d != 64 && c->d != 128) return fail(SPARGE_EUNSUPPORTED, "head dim %d not supported (64 or 128)", c->d);
+    if (c->dtype != SPARGE_F16 && c->dtype != SPARGE_BF16) return fail(SPARGE_EUNSUPPORTED, "dtype %d not supported", c->dtype);
+    if (c->R > SPARGE_CACHE_MAX_ROWS) return fail(SPARGE_EUNSUPPORTED, "R = %d exceeds %d", c->R, SPARGE_CACHE_MAX_ROWS);
+    if (c->H_kv > SPARGE_MAX_HEADS) return fail(SPARGE_EUNSUPPORTED, "H_kv = %d exceeds %d", c->H_kv, SPARGE_MAX_HEADS);
+    if (c->n_pages > 1 << 24 || c->max_blocks > 1 << 24) return fail(SPARGE_EUNSUPPORTED, "n_pages and max_blocks must not exceed 2^24");
+    if (table && (!c->table || off4(c->table))) return fail(SPARGE_EINVAL, "table must be 4-byte aligned device memory");
+    return SPARGE_OK;
+}
+
+int check_pages(const sparge_cache* c) {
+    if (!c->k || !c->v || !c->k_amax || !c->v_amax) return fail(SPARGE_EINVAL, "NULL page array");
+    if (misaligned(c->k) || misaligned(c->v) || misaligned(c->k_shift)) return fail(SPARGE_EINVAL, "k, v, k_shift must be 16-byte aligned");
+    if (off4(c->k_amax) || off4(c->v_amax)) return fail(SPARGE_EINVAL, "k_amax and v_amax must be 4-byte aligned");
+    return SPARGE_OK;
+}
+
+int check_query_heads(const sparge_cache* c, int H) {
+    if (H < 1 || H % c->H_kv) return fail(SPARGE_EINVAL, "H = %d is not a multiple of H_kv = %d", H, c->H_kv);
+    if (H > SPARGE_MAX_HEADS) return fail(SPARGE_EUNSUPPORTED, "H = %d exceeds %d", H, SPARGE_MAX_HEADS);
+    return SPARGE_OK;
+}
+
+int check_slots(int n) {
+    if (n < 0) return fail(SPARGE_EINVAL, "n_slots = %d is negative", n);
+    if (n > 1 << 30) return fail(SPARGE_EUNSUPPORTED, "n_slots = %d exceeds 2^30", n);
+    return SPARGE_OK;
+}
+
+int check_token_strides(int64_t n, int64_t h) {
+    if (n < 0 || h < 0) return fail(SPARGE_EINVAL, "bad strides");
+    if (n % 8 || h % 8) return fail(SPARGE_EINVAL, "strides must be multiples of 8 elements");
+    return SPARGE_OK;
+}
 
 // Partition of the scratch buffer.  Every entry point uses a subset; offsets are fixed by shape.
 struct Workspace {
@@ -900,6 +940,87 @@ int sparge_permute_tokens(const void* src, const sparge_desc* desc, const int32_
         return fail(SPARGE_EINVAL, "tokens [%d, %d) do not lie inside N = %d", offset, offset + L, s.N);
     hipError_t e = launch_permute_tokens(src, s, perm, L, offset, inverse, dst, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? SPARGE_OK : hip_fail(e, "permute_tokens");
+}
+
+int sparge_cache_plan(const sparge_cache* cache, const int32_t* new_len, const uint8_t* release, int n_slots, int32_t* cu,
+                      int32_t* slots, int32_t* req, int32_t* status, void* hip_stream) {
+    int rc = check_cache(cache, true);
+    if (rc) return rc;
+    if (!cache->length || !cache->free_pages || !cache->n_free || !new_len || !cu || !status) return fail(SPARGE_EINVAL, "NULL argument");
+    if ((rc = check_slots(n_slots))) return rc;
+    if (n_slots > 0 && (!slots || !req)) return fail(SPARGE_EINVAL, "slots or req is NULL");
+    if (off4(new_len) || off4(cu) || off4(slots) || off4(req) || off4(status) || off4(cache->length) || off4(cache->free_pages) || off4(cache->n_free))
+        return fail(SPARGE_EINVAL, "int32 arrays must be 4-byte aligned");
+    hipError_t e = launch_cache_plan(*cache, new_len, release, n_slots, cu, slots, req, status, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? SPARGE_OK : hip_fail(e, "cache_plan");
+}
+
+int sparge_cache_append(const sparge_cache* cache, const void* K, const void* V, int n_slots, int64_t k_stride_n,
+                        int64_t k_stride_h, int64_t v_stride_n, int64_t v_stride_h, const int32_t* cu, const int32_t* slots,
+                        const int32_t* req, void* hip_stream) {
+    int rc = check_cache(cache, false);
+    if (rc || (rc = check_pages(cache))) return rc;
+    if (!cache->k_tail || !cache->v_tail || misaligned(cache->k_tail) || misaligned(cache->v_tail))
+        return fail(SPARGE_EINVAL, "k_tail and v_tail must be 16-byte aligned device memory");
+    if ((rc = check_slots(n_slots))) return rc;
+    if (n_slots == 0) return SPARGE_OK;
+    if (!K || !V || !cu || !slots || !req) return fail(SPARGE_EINVAL, "NULL argument");
+    if (misaligned(K) || misaligned(V)) return fail(SPARGE_EINVAL, "tensor pointers must be 16-byte aligned");
+    if (off4(cu) || off4(slots) || off4(req)) return fail(SPARGE_EINVAL, "int32 arrays must be 4-byte aligned");
+    if ((rc = check_token_strides(k_stride_n, k_stride_h)) || (rc = check_token_strides(v_stride_n, v_stride_h))) return rc;
+    hipError_t e = launch_cache_append(*cache, K, V, n_slots, k_stride_n, k_stride_h, v_stride_n, v_stride_h, cu, slots, req,
+                                       static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? SPARGE_OK : hip_fail(e, "cache_append");
+}
+
+int sparge_cache_read(const sparge_cache* cache, const int32_t* slots, const int32_t* req, int n_slots, int out_dtype, void* K,
+                      void* V, void* hip_stream) {
+    int rc = check_cache(cache, false);
+    if (rc || (rc = check_pages(cache))) return rc;
+    if (out_dtype != SPARGE_F32 && out_dtype != cache->dtype)
+        return fail(SPARGE_EUNSUPPORTED, "output type %d is neither SPARGE_F32 nor the cache's type %d", out_dtype, cache->dtype);
+    if ((rc = check_slots(n_slots))) return rc;
+    if (n_slots == 0) return SPARGE_OK;
+    if (!K || !V || !slots) return fail(SPARGE_EINVAL, "NULL argument");
+    if (cache->k_shift && !req) return fail(SPARGE_EINVAL, "a cache with k_shift needs req");
+    if (misaligned(K) || misaligned(V)) return fail(SPARGE_EINVAL, "tensor pointers must be 16-byte aligned");
+    if (off4(slots) || off4(req)) return fail(SPARGE_EINVAL, "int32 arrays must be 4-byte aligned");
+    hipError_t e = launch_cache_read(*cache, slots, req, n_slots, out_dtype, K, V, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? SPARGE_OK : hip_fail(e, "cache_read");
+}
+
+int sparge_cache_attn_workspace_bytes(const sparge_cache* cache, int H, size_t* bytes) {
+    int rc = check_cache(cache, false);
+    if (rc || (rc = check_query_heads(cache, H))) return rc;
+    if (!bytes) return fail(SPARGE_EINVAL, "bytes is NULL");
+    *bytes = cache_attn_workspace(cache->d);
+    return SPARGE_OK;
+}
+
+int sparge_cache_attn(const sparge_cache* cache, const void* Q, int n_slots, int H, int64_t q_stride_n, int64_t q_stride_h,
+                      const int32_t* cu, const uint8_t* mask, float sm_scale, int causal, void* O, int64_t o_stride_n,
+                      int64_t o_stride_h, void* ws, size_t ws_bytes, void* hip_stream) {
+    int rc = check_cache(cache, true);
+    if (rc || (rc = check_pages(cache)) || (rc = check_query_heads(cache, H))) return rc;
+    if (!cache->length || off4(cache->length)) return fail(SPARGE_EINVAL, "length must be 4-byte aligned device memory");
+    if ((rc = check_slots(n_slots))) return rc;
+    if (n_slots == 0) return SPARGE_OK;
+    if (!Q || !O || !cu) return fail(SPARGE_EINVAL, "NULL argument");
+    if (misaligned(Q) || misaligned(O)) return fail(SPARGE_EINVAL, "tensor pointers must be 16-byte aligned");
+    if (off4(cu)) return fail(SPARGE_EINVAL, "cu must be 4-byte aligned");
+    if ((rc = check_token_strides(q_stride_n, q_stride_h)) || (rc = check_token_strides(o_stride_n, o_stride_h))) return rc;
+    if ((n_slots > 1 && o_stride_n < cache->d) || (H > 1 && o_stride_h < cache->d)) return fail(SPARGE_EINVAL, "rows of O must not overlap");
+    if (!(sm_scale < INFINITY)) return fail(SPARGE_EINVAL, "sm_scale must be finite");
+    const size_t need = cache_attn_workspace(cache->d);
+    if (!ws || reinterpret_cast<uintptr_t>(ws) % 256) return fail(SPARGE_EINVAL, "workspace must be 256-byte aligned device memory");
+    if (ws_bytes < need) return fail(SPARGE_ENOSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
+    CacheAttn a;
+    a.n_slots = n_slots, a.H = H, a.causal = causal != 0;
+    a.q_sn = q_stride_n, a.q_sh = q_stride_h, a.o_sn = o_stride_n, a.o_sh = o_stride_h;
+    a.cu = cu, a.mask = mask;
+    a.scale_log2 = (sm_scale > 0.f ? sm_scale : 1.0f / std::sqrt(static_cast<float>(cache->d))) * 1.4426950408889634f;
+    hipError_t e = launch_cache_attn(*cache, a, Q, O, ws, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? SPARGE_OK : hip_fail(e, "cache_attn");
 }
 
 int sparge_set_timing_events(void* const* starts, void* const* stops, int n) {

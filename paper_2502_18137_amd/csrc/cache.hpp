@@ -1,0 +1,50 @@
+// Internal declarations of the paged 8-bit K/V cache: plan, append, read-back, attention over it.
+#pragma once
+#include "common.hpp"
+
+namespace sparge {
+
+// A page holds 64 tokens per kv head, K and V each as 64 d bytes in the operand order of the 16x16x32 MFMA, so that the
+// attention loads its operands straight into registers, 1 KB of consecutive bytes per wave and load.  A byte is code + 128.
+//   K: [key / 16][channel / 64][key % 16 + 16 (channel % 64 / 16)][channel % 16]
+//   V: [channel / 16][channel % 16 + 16 (key % 16 / 4)][4 (key / 16) + key % 4]
+// (the V order is the one in which the accumulators of K Q^T hand a lane its keys).
+constexpr int PAGE = SPARGE_CACHE_PAGE;
+static_assert(PAGE == 64, "the layouts, a ballot per page of a window and the attention's tiles are made for 64");
+
+__host__ __device__ inline int k_byte(int key, int ch, int d) {
+    return (((key >> 4) * (d >> 6) + (ch >> 6)) * 64 + (key & 15) + 16 * ((ch >> 4) & 3)) * 16 + (ch & 15);
+}
+__host__ __device__ inline int v_byte(int key, int ch) {
+    return ((ch >> 4) * 64 + (ch & 15) + 16 * ((key >> 2) & 3)) * 16 + 4 * (key >> 4) + (key & 3);
+}
+
+// One attention call: what the host knows of it.
+struct CacheAttn {
+    int n_slots, H, causal;
+    long long q_sn, q_sh, o_sn, o_sh;   // element strides
+    const int32_t* cu;
+    const uint8_t* mask;                // [R, H_kv, max_blocks] or null
+    float scale_log2;                   // softmax scale times log2 e
+};
+
+// Workgroups of the attention launch, each with an equal share of the call's work; the workspace holds up to two partial
+// results of each and what the joining launch has to know.
+constexpr int CACHE_WGS = 512;
+constexpr int CACHE_WG_ROWS = 128;      // query rows that a workgroup takes at most
+struct JoinDesc {
+    int n_parts;                        // 0: nothing to join here
+    int part, row, head, tile;          // the part whose beginning is the first boundary inside the item; the item
+};
+size_t cache_attn_workspace(int d);
+
+hipError_t launch_cache_plan(const sparge_cache& c, const int32_t* new_len, const uint8_t* release, int n_slots, int32_t* cu,
+                             int32_t* slots, int32_t* req, int32_t* status, hipStream_t st);
+hipError_t launch_cache_append(const sparge_cache& c, const void* K, const void* V, int n_slots, long long k_sn, long long k_sh,
+                               long long v_sn, long long v_sh, const int32_t* cu, const int32_t* slots, const int32_t* req,
+                               hipStream_t st);
+hipError_t launch_cache_read(const sparge_cache& c, const int32_t* slots, const int32_t* req, int n_slots, int out_dtype, void* K,
+                             void* V, hipStream_t st);
+hipError_t launch_cache_attn(const sparge_cache& c, const CacheAttn& a, const void* Q, void* O, void* ws, hipStream_t st);
+
+}  // namespace sparge
