@@ -28,10 +28,7 @@ struct CacheAttn {
     float scale_log2;                   // softmax scale times log2 e
 };
 
-// Workgroups of the attention launch, each with an equal share of the call's work; the workspace holds up to two partial
-// results of each and what the joining launch has to know.
-constexpr int CACHE_WGS = 512;
-constexpr int CACHE_WG_ROWS = 128;      // query rows that a workgroup takes at most
+// What the joining launch has to know of a part of the attention's work.
 struct JoinDesc {
     int n_parts;                        // 0: nothing to join here
     int part, row, head, tile;          // the part whose beginning is the first boundary inside the item; the item

@@ -4,15 +4,17 @@
 // block's scales sk, sv: q_i . k_j = sk (q_i . a_j) and v_j = sv b_j.  Both products run on the 16-bit MFMA with the codes as
 // fp16 integers (exact), S^T = A Q^T and O^T = B^T P^T, so that a lane owns one query (lane % 16) and four keys of every
 // sixteen, and P goes from the accumulators of the first product to the operand of the second without leaving the lane:
-// the pages' byte order is made for that, and operands are loaded from memory into registers, 1 KB per wave and load,
-// without LDS.  sk enters the exponent; sv enters p before it is rounded, relative to the largest sv so far, to which O
-// is kept relative.
+// the pages' byte order is made for that.  sk enters the exponent; sv enters p before it is rounded, relative to the
+// largest sv so far, to which O is kept relative.
 //
-// Work: an item is a kv head's group of up to 64 QT query rows (tokens x grouped heads) of one row of the cache, weighed by the keys
-// it sees and the waves it needs.  The items lie one behind the other on a line that is cut into equal parts, one per
-// workgroup: a long item is split over several, whose partial results a second launch joins in a fixed order, and a
-// short one shares a workgroup with others.  Where the rows of an item fit 16 QT (32 QT), its four (two) waves take
-// every fourth (second) kept block instead of rows.
+// The query rows of one row of the cache are its new tokens times the G heads that share a kv head.  Two kernels:
+//   rows of at most 16 query rows (decoding): the work is reading pages.  A wave takes blocks by itself, operands come
+//   from memory into registers, 1 KB of consecutive bytes a load, without LDS and without barriers.
+//   rows of more: the work is products.  Four waves take 32 query rows each and share the blocks, which they convert to
+//   fp16 into LDS once, a quarter each.
+// In both, items (a kv head's tile of query rows) lie one behind the other on a line, each as long as the keys it sees; the
+// line is cut into equal parts, one per wave or workgroup.  A long item is split over several parts, whose results a
+// further launch joins in a fixed order; short ones share a part.
 #include "cache.hpp"
 
 namespace sparge {
@@ -26,8 +28,13 @@ typedef unsigned long long u64;
 constexpr float FAR = -1e30f;          // reference of a row that has seen no key
 constexpr float SLACK = 4.0f;          // log2: how far a row's maximum may run ahead of the reference inside exp2
 constexpr float SV_SLACK = 4.0f;       // how far a block's V scale may exceed the one that O is relative to
-constexpr float P_UP = 256.0f;         // p is at most 2^4, its factor sv ratio at most 4: p x ratio x 2^8 <= 2^14 in fp16, and
+constexpr float P_UP_LOG2 = 8.0f;      // p is at most 2^4, its factor sv ratio at most 4: p x ratio x 2^8 <= 2^14 in fp16, and
                                        // weights down to 2^-33 of the largest are not lost
+constexpr float SV_LEAST = 0x1p-60f;   // smaller ratios (and blocks of zeros) count as this: below every rounding beside sv_ref
+
+constexpr int NARROW_ROWS = 16, NARROW_WGS = 512, NARROW_PARTS = 4 * NARROW_WGS;   // two workgroups per compute unit
+constexpr int WIDE_QT = 2, WIDE_ROWS = 64 * WIDE_QT, WIDE_WGS = 512;
+constexpr int JOIN_Y = 4;              // workgroups among which an item's rows are dealt out
 
 template <int X>
 __device__ __forceinline__ float other(float v) {   // of lane ^ X, X = 16 or 32
@@ -48,6 +55,10 @@ __device__ __forceinline__ float sum_groups(float v) {
     v += other<16>(v);
     return v + other<32>(v);
 }
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ u64 uniform(u64 v) {
+    return static_cast<u64>(uniform(static_cast<int>(v >> 32))) << 32 | static_cast<uint32_t>(uniform(static_cast<int>(v)));
+}
 
 // 8 bytes (code + 128) -> 8 fp16 codes: the byte under 0x64 is the fp16 1024 + byte, less 1152 the code, all exact
 __device__ __forceinline__ v8h codes8(uint32_t a, uint32_t b) {
@@ -65,7 +76,8 @@ __device__ __forceinline__ v8h codes8(uint32_t a, uint32_t b) {
     return r;
 }
 
-// How a row of the cache is cut: Gp grouped heads a tile holds (the group, or a part of it where it exceeds a workgroup), TT tokens.
+// How a row's query rows are cut into tiles of up to `rows`: TT whole tokens of Gp heads, or, where a token's group exceeds a
+// tile, `parts` pieces of the group.
 struct Cut {
     int G, Gp, parts, TT;
 };
@@ -74,75 +86,461 @@ __host__ __device__ inline Cut cut_of(int G, int rows) {
     return {G, rows, (G + rows - 1) / rows, 1};
 }
 
+// Which rows a launch takes: all, those of at most 16 query rows, or the others.
+enum Rows { ALL_ROWS, FEW_ROWS, MANY_ROWS };
+
 struct RowInfo {
-    int first, n, len, p0;     // new tokens [first, first + n), keys, keys before the first new token
-    int tiles, rg;             // tiles of TT tokens; waves over rows
-    u64 chunk;                 // weight of one kv head's part
+    int first, n, len, p0;     // new tokens [first, first + n) (0: not this launch's), keys, keys before the first new token
+    int tiles;                 // tiles of TT tokens
 };
+__device__ __forceinline__ RowInfo row_info(const sparge_cache& c, const CacheAttn& a, const Cut& t, Rows which, int r) {
+    RowInfo x;
+    x.first = max(0, min(a.cu[r], a.n_slots));
+    x.n = max(0, min(a.cu[r + 1], a.n_slots) - x.first);
+    x.len = max(0, min(c.length[r], static_cast<int>(min(static_cast<long long>(c.max_blocks) * PAGE, 0x7FFFFFC0ll))));
+    x.p0 = max(0, x.len - x.n);
+    if (which != ALL_ROWS && (static_cast<long long>(x.n) * t.G <= NARROW_ROWS) != (which == FEW_ROWS)) x.n = 0;
+    x.tiles = (x.n + t.TT - 1) / t.TT;
+    return x;
+}
+__device__ __forceinline__ RowInfo uniform(RowInfo x) {
+    x.first = uniform(x.first), x.n = uniform(x.n), x.len = uniform(x.len), x.p0 = uniform(x.p0), x.tiles = uniform(x.tiles);
+    return x;
+}
+
+struct Joint {                          // workspace
+    JoinDesc* desc;                     // [parts]
+    float* ml;                          // [2 parts][rows of a tile][2] reference and sum of a row's part
+    float* o;                           // [2 parts][rows of a tile][d]
+};
+
+// exclusive prefix of v over the 256 threads and the total; lds: 4 values
+__device__ __forceinline__ u64 prefix(u64 v, u64* lds, u64& total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    u64 upto = v;
+    for (int s = 1; s < 64; s <<= 1) {
+        const u64 x = __shfl_up(upto, s);
+        if (lane >= s) upto += x;
+    }
+    if (lane == 63) lds[wave] = upto;
+    __syncthreads();
+    total = 0;
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) upto += lds[w];
+        total += lds[w];
+    }
+    return upto - v;
+}
+
+// Where a part begins inside an item: what the join needs.  start, end: the item on the line.
+__device__ __forceinline__ JoinDesc boundary(u64 total, int parts, int part, u64 start, u64 end, int row, int head, int tile) {
+    if (total * (part - 1) / parts > start) return {0, 0, 0, 0, 0};          // not the item's first boundary
+    const u64 last = (end * parts + total - 1) / total - 1;                   // its last one
+    return {static_cast<int>(last) - part + 2, part, row, head, tile};
+}
+
+// The blocks of an item's range, 64 table entries at a time, one a lane, the next 64 on their way.
+struct Blocks {
+    int base, end, next_page, l_page;
+    float l_ka, l_va;
+    u64 bits;
+    const int32_t* table;
+    const uint8_t* mask;
+
+    __device__ __forceinline__ void ahead(int j) {   // a page, or -1: not there or not kept
+        next_page = -1;
+        if (j < end && (!mask || mask[j])) next_page = table[j];
+    }
+    __device__ __forceinline__ void open(const sparge_cache& c, const CacheAttn& a, int r, int kh, int b0, int b1) {
+        base = b0 - 64, end = b1, bits = 0;
+        table = c.table + static_cast<long long>(r) * c.max_blocks;
+        mask = a.mask ? a.mask + (static_cast<long long>(r) * c.H_kv + kh) * c.max_blocks : nullptr;
+        ahead(b0 + static_cast<int>(threadIdx.x & 63));
+    }
+    // at: the lane that holds the block's page and scales
+    __device__ __forceinline__ bool next(const sparge_cache& c, int kh, int& block, int& page, int& at) {
+        while (bits == 0) {
+            base += 64;
+            if (base >= end) return false;
+            l_page = next_page;
+            const bool keep = l_page >= 0 && l_page < c.n_pages;
+            if (keep) {
+                l_ka = c.k_amax[static_cast<long long>(l_page) * c.H_kv + kh];
+                l_va = c.v_amax[static_cast<long long>(l_page) * c.H_kv + kh];
+            }
+            ahead(base + 64 + static_cast<int>(threadIdx.x & 63));
+            bits = __ballot(keep);
+        }
+        at = __builtin_ctzll(bits);
+        bits &= bits - 1;
+        block = base + at;
+        page = __builtin_amdgcn_readlane(l_page, at);
+        return true;
+    }
+    __device__ __forceinline__ float ka(int at) const { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l_ka), at)); }
+    __device__ __forceinline__ float va(int at) const { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l_va), at)); }
+};
+
+// A tile of 16 query rows as an MFMA operand: fp16 as it is; bf16 times the power of two that brings the row's largest to [1, 2)
+// (exact but for what is below 2^-24 of it).  Operand s holds channels 64 (s / 2) + 16 (lane / 16) + 8 (s % 2) + 0..7.
+template <int D>
+__device__ __forceinline__ void load_q(uint4 (&raw)[D / 32], const uint16_t* row, bool valid) {
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+        raw[s] = make_uint4(0u, 0u, 0u, 0u);
+        if (valid) raw[s] = *reinterpret_cast<const uint4*>(row + 64 * (s >> 1) + 8 * (s & 1));
+    }
+}
+template <int D, int DT>
+__device__ __forceinline__ float convert_q(const uint4 (&raw)[D / 32], v8h (&qf)[D / 32]) {
+    if constexpr (DT == SPARGE_F16) {
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) __builtin_memcpy(&qf[s], &raw[s], 16);
+        return 1.0f;
+    } else {
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7FFFu, (w[e] >> 16) & 0x7FFFu));
+        }
+        top = max(top, __float_as_uint(other<16>(__uint_as_float(top))));
+        top = max(top, __float_as_uint(other<32>(__uint_as_float(top))));
+        int ex = static_cast<int>(top >> 7) - 127;          // exponent of the largest (top: bf16 bits)
+        if (ex > 127 || top == 0) ex = 0;                   // NaN and infinity stay what they are
+        const float down = __builtin_ldexpf(1.0f, -ex);
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                qf[s][2 * e] = static_cast<_Float16>(cvt16<DT>(static_cast<uint16_t>(w[e] & 0xFFFFu)) * down);
+                qf[s][2 * e + 1] = static_cast<_Float16>(cvt16<DT>(static_cast<uint16_t>(w[e] >> 16)) * down);
+            }
+        }
+        return __builtin_ldexpf(1.0f, ex);
+    }
+}
+
+// V's scale of a block against the one that O is relative to: the factor's log2 (with P_UP_LOG2) and inverse.
+struct VScale {
+    float ref = 0.f, f_log2, f_inv;
+
+    // -> what O has to be multiplied with first (1: nothing)
+    __device__ __forceinline__ float take(float va) {
+        float down = 1.0f;
+        if (va > SV_SLACK * ref && va < INFINITY) down = ref / va, ref = va;
+        float f = va / ref;                          // (NaN and infinity stay; 0 / 0: codes are 0)
+        if (va < SV_LEAST * ref || va == 0.f) f = SV_LEAST;
+        f_log2 = __builtin_amdgcn_logf(f) + P_UP_LOG2, f_inv = __builtin_amdgcn_rcpf(f) * 0x1p-8f;
+        return down;
+    }
+};
+
+// One tile's softmax step on a block's scores s (keys 16 t + 4 (lane / 16) + e): the weights times V's factor as operand pf,
+// the row's reference m and sum l, O scaled where the reference moves.  last: the last key of the block that the row sees,
+// less 4 (lane / 16); looked at only if `masked`.
+template <int NV>
+__device__ __forceinline__ void softmax(v4f (&s)[4], float cq, const VScale& v, bool masked, int last, float& m, float& l,
+                                        v4f (&o)[NV], v8h (&pf)[2]) {
+    if (cq == 0.f) cq = 1e-37f;   // a block of zeros: -inf below stays what it is
+    if (masked) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (16 * t + e > last) s[t][e] = -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[t][e]);
+    top = max_groups(top) * cq;
+    if (__any(top > m + SLACK)) {
+        const float to = fmaxf(m, top), down = __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= down;
+#pragma unroll
+        for (int n = 0; n < NV; ++n) o[n] *= down;
+    }
+    float w[16];
+    const float from = v.f_log2 - m;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * t + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], cq, from));
+    if (masked) {   // a key that is not seen has no weight even where the block's scales are NaN or infinite
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (16 * t + e > last) w[4 * t + e] = 0.f;
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum += w[e];
+    l += masked && sum == 0.f ? 0.f : sum * v.f_inv;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = static_cast<_Float16>(w[e]);
+}
+
+// A tile's rows, whole (divided by their sums) or as a part.
+template <int NV, int DT>
+__device__ __forceinline__ void store_whole(const v4f (&o)[NV], float l, float o_scale, uint16_t* out) {
+    const float inv = o_scale / l;
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+        uint16_t h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = l == 0.f ? 0 : cvt_to16<DT>(o[n][e] * inv);
+        uint2 w;
+        __builtin_memcpy(&w, h, 8);
+        *reinterpret_cast<uint2*>(out + 16 * n) = w;
+    }
+}
+template <int NV>
+__device__ __forceinline__ void store_part(const v4f (&o)[NV], float m, float l, float o_scale, const Joint& ws, long long at) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int n = 0; n < NV; ++n) *reinterpret_cast<v4f*>(ws.o + at * (16 * NV) + 16 * n + 4 * (lane >> 4)) = o[n] * o_scale;
+    if (lane < 16) ws.ml[2 * at] = m, ws.ml[2 * at + 1] = l;
+}
+
+// ---- few query rows: a wave by itself ------------------------------------------------------------------------------
+
+// Bound by the pages' bytes: a wave keeps the next block's K and V on their way while it works on one, 16 KB (d = 128), eight
+// waves on a compute unit; and it looks ahead over the end of an item, so that the next one's table, queries and first block
+// come while the last block of this one is worked on.
+template <int D, int DT>
+__global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache c, CacheAttn a, Rows which, const uint16_t* __restrict__ Q,
+                                                                   uint16_t* __restrict__ O, Joint ws) {
+    constexpr int NK = 4 * D / 64, NV = D / 16, KS = D / 32;
+    __shared__ u64 sums[4];
+    __shared__ u64 found_rem[4];
+    __shared__ int found_row[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const Cut cut = cut_of(a.H / c.H_kv, NARROW_ROWS);
+    const int heads = c.H_kv * cut.parts;
+
+    // ---- this wave's part of the line, in blocks.  (All tiles of a row count with all its blocks: they are few here.)
+    const int per = (c.R + 255) / 256;
+    auto length_of = [&](const RowInfo& x) { return static_cast<u64>(x.tiles) * heads * ((x.len + PAGE - 1) / PAGE); };
+    u64 mine = 0, total;
+    for (int r = tid * per; r < min((tid + 1) * per, c.R); ++r) mine += length_of(row_info(c, a, cut, which, r));
+    const u64 before = prefix(mine, sums, total);
+    const int parts = static_cast<int>(min(total, static_cast<u64>(NARROW_PARTS)));
+    const int part = static_cast<int>(blockIdx.x) * 4 + wave;
+    for (int w = 0; w < 4; ++w) {
+        const int p = static_cast<int>(blockIdx.x) * 4 + w;
+        if (p >= parts) break;
+        const u64 at = total * p / parts;
+        if (before <= at && at < before + mine) {
+            u64 rem = at - before;
+            int r = tid * per;
+            for (; r < c.R - 1; ++r) {
+                const u64 all = length_of(row_info(c, a, cut, which, r));
+                if (rem < all) break;
+                rem -= all;
+            }
+            found_row[w] = r;
+            found_rem[w] = rem;
+        }
+    }
+    __syncthreads();
+    if (part >= parts) {
+        if (lane == 0) ws.desc[part].n_parts = 0;
+        return;
+    }
+    const u64 lo = uniform(total * part / parts);
+    u64 left = uniform(total * (part + 1) / parts) - lo;     // blocks that this wave still has to take
+    u64 rem = uniform(found_rem[wave]);                       // where in row `r` the next ones begin
+    int r = uniform(found_row[wave]);
+    bool first_item = true;
+
+    struct Item {
+        RowInfo x;
+        int row, kh, gpart, tile, ntok, b0, b1, blocks;
+    };
+    auto next_item = [&](Item& it) -> bool {
+        while (left > 0 && r < c.R) {
+            it.x = uniform(row_info(c, a, cut, which, r));
+            it.blocks = (it.x.len + PAGE - 1) / PAGE;
+            const u64 all = length_of(it.x);
+            if (rem >= all) {
+                rem -= all;
+                ++r;
+                continue;
+            }
+            const uint32_t tile = static_cast<uint32_t>(rem / static_cast<uint32_t>(it.blocks));   // of all heads' tiles
+            it.b0 = static_cast<int>(rem - static_cast<u64>(tile) * it.blocks);
+            const int head = static_cast<int>(tile / static_cast<uint32_t>(it.x.tiles));
+            it.tile = static_cast<int>(tile - static_cast<uint32_t>(head) * it.x.tiles);
+            it.row = r, it.kh = head / cut.parts, it.gpart = head - it.kh * cut.parts;
+            it.ntok = min(cut.TT, it.x.n - it.tile * cut.TT);
+            const u64 take = min(static_cast<u64>(it.blocks - it.b0), left);
+            it.b1 = it.b0 + static_cast<int>(take);
+            if (first_item) {
+                JoinDesc d = {0, 0, 0, 0, 0};
+                if (it.b0 > 0) d = boundary(total, parts, part, lo - it.b0, lo - it.b0 + it.blocks, r, head, it.tile);
+                if (lane == 0) ws.desc[part] = d;
+                first_item = false;
+            }
+            left -= take;
+            rem += take;
+            return true;
+        }
+        return false;
+    };
+
+    Blocks blocks;
+    uint4 q_raw[KS], kraw[NK], vraw[NV];
+    int limit = -1, lim_lo = -1;        // of the item whose queries are in q_raw: the lane's row; the least of all rows
+    int out_token = 0, out_head = 0;    // the lane's row of Q and O
+    bool valid = false;
+    auto open = [&](const Item& it) {
+        const int row = lane & 15, tok = row / cut.Gp, g = it.gpart * NARROW_ROWS + row - tok * cut.Gp;
+        valid = tok < it.ntok && g < cut.G;
+        const int t = it.tile * cut.TT;
+        limit = !valid ? -1 : a.causal ? min(it.x.p0 + t + tok, it.x.len - 1) : it.x.len - 1;
+        lim_lo = a.causal ? min(it.x.p0 + t, it.x.len - 1) : it.x.len - 1;
+        const int lim_hi = a.causal ? min(it.x.p0 + t + it.ntok - 1, it.x.len - 1) : it.x.len - 1;
+        blocks.open(c, a, it.row, it.kh, it.b0, min(it.b1, lim_hi / PAGE + 1));
+        out_token = it.x.first + t + tok, out_head = it.kh * cut.G + g;
+        load_q<D>(q_raw, Q + out_token * a.q_sn + out_head * a.q_sh + 16 * (lane >> 4), valid);
+    };
+    auto load_k = [&](int page, int kh) {
+        const uint8_t* p = static_cast<const uint8_t*>(c.k) + (static_cast<long long>(page) * c.H_kv + kh) * (PAGE * D) + lane * 16;
+#pragma unroll
+        for (int n = 0; n < NK; ++n) kraw[n] = *reinterpret_cast<const uint4*>(p + n * 1024);
+    };
+    auto load_v = [&](int page, int kh) {
+        const uint8_t* p = static_cast<const uint8_t*>(c.v) + (static_cast<long long>(page) * c.H_kv + kh) * (PAGE * D) + lane * 16;
+#pragma unroll
+        for (int n = 0; n < NV; ++n) vraw[n] = *reinterpret_cast<const uint4*>(p + n * 1024);
+    };
+
+    Item it;
+    bool have = next_item(it), more = false;
+    int block = 0, page = 0, at = 0;
+    if (!have && lane == 0) ws.desc[part].n_parts = 0;
+    if (have) {
+        open(it);
+        more = blocks.next(c, it.kh, block, page, at);
+        if (more) {
+            load_k(page, it.kh);
+            load_v(page, it.kh);
+        }
+    }
+    while (have) {
+        v8h qf[KS];
+        const float qs = a.scale_log2 * convert_q<D, DT>(q_raw, qf);
+        const int my_limit = limit - 4 * (lane >> 4), all_limit = lim_lo;
+        const int my_token = out_token, my_head = out_head;
+        const bool mine_valid = valid;
+        v4f o[NV];
+        float m = FAR, l = 0.f;
+        VScale vs;
+#pragma unroll
+        for (int n = 0; n < NV; ++n) o[n] = {0.f, 0.f, 0.f, 0.f};
+        Item nx;
+        bool n_have = false, asked = false, n_more = false;
+        int n_block = 0, n_page = 0, n_at = 0;
+        while (true) {
+            v4f s[4];
+            float ka = 0.f, va = 0.f;
+            if (more) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    s[t] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < D / 64; ++e) {
+                        const uint4 w = kraw[t * (D / 64) + e];
+                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(w.x, w.y), qf[2 * e], s[t], 0, 0, 0);
+                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(w.z, w.w), qf[2 * e + 1], s[t], 0, 0, 0);
+                    }
+                }
+                ka = blocks.ka(at), va = blocks.va(at);
+            }
+            // the next block: of this item, else of the next one
+            n_more = blocks.next(c, it.kh, n_block, n_page, n_at);
+            int n_kh = it.kh;
+            if (!n_more) {
+                asked = true;
+                n_have = next_item(nx);
+                if (n_have) {
+                    n_kh = nx.kh;
+                    open(nx);
+                    n_more = blocks.next(c, n_kh, n_block, n_page, n_at);
+                }
+            }
+            if (n_more) load_k(n_page, n_kh);
+            if (more) {
+                const float down = vs.take(va);
+                if (down != 1.0f) {
+#pragma unroll
+                    for (int n = 0; n < NV; ++n) o[n] *= down;
+                }
+                v8h pf[2];
+                softmax<NV>(s, qs * (ka * (1.0f / 127.0f)), vs, block * PAGE + PAGE - 1 > all_limit, my_limit - block * PAGE, m, l, o, pf);
+#pragma unroll
+                for (int n = 0; n < NV; ++n) {
+                    o[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(vraw[n].x, vraw[n].y), pf[0], o[n], 0, 0, 0);
+                    o[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(vraw[n].z, vraw[n].w), pf[1], o[n], 0, 0, 0);
+                }
+            }
+            if (n_more) load_v(n_page, n_kh);
+            more = n_more, block = n_block, page = n_page, at = n_at;
+            if (asked) break;
+        }
+        l = sum_groups(l);
+        if (mine_valid) {
+            const float o_scale = vs.ref * (1.0f / (127.0f * 256.0f));
+            if (it.b0 == 0 && it.b1 == it.blocks) {
+                store_whole<NV, DT>(o, l, o_scale, O + my_token * a.o_sn + my_head * a.o_sh + 4 * (lane >> 4));
+            } else {
+                store_part<NV>(o, m, l, o_scale, ws, static_cast<long long>(2 * part + (it.b0 > 0 ? 0 : 1)) * NARROW_ROWS + (lane & 15));
+            }
+        }
+        it = nx;
+        have = n_have;
+    }
+}
+
+// ---- many query rows: four waves share the blocks --------------------------------------------------------------------
+
 __device__ __forceinline__ u64 sum_vis(const RowInfo& x, const Cut& t, bool causal, int i) {   // keys that the tiles before i see
     if (!causal) return static_cast<u64>(i) * x.len;
     u64 s = static_cast<u64>(i) * x.p0 + static_cast<u64>(t.TT) * i * (i + 1) / 2;
     if (i == x.tiles) s -= static_cast<u64>(x.tiles) * t.TT - x.n;   // the last tile may hold fewer tokens
     return s;
 }
-template <int QT>
-__device__ __forceinline__ RowInfo row_info(const sparge_cache& c, const CacheAttn& a, const Cut& t, int r) {
-    RowInfo x;
-    x.first = max(0, min(a.cu[r], a.n_slots));
-    x.n = max(0, min(a.cu[r + 1], a.n_slots) - x.first);
-    x.len = max(0, min(c.length[r], static_cast<int>(min(static_cast<long long>(c.max_blocks) * PAGE, 0x7FFFFFC0ll))));
-    x.p0 = max(0, x.len - x.n);
-    x.tiles = (x.n + t.TT - 1) / t.TT;
-    const int rows = min(x.n, t.TT) * t.Gp;
-    x.rg = rows <= 16 * QT ? 1 : rows <= 32 * QT ? 2 : 4;
-    x.chunk = x.rg * sum_vis(x, t, a.causal, x.tiles);
-    return x;
-}
 
-__device__ __forceinline__ u64 uniform(u64 v) {
-    return static_cast<u64>(__builtin_amdgcn_readfirstlane(static_cast<int>(v >> 32))) << 32 |
-           static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v)));
-}
-
-struct Joint {                          // workspace
-    JoinDesc* desc;                     // [CACHE_WGS]
-    float* ml;                          // [2 CACHE_WGS][CACHE_WG_ROWS][2] reference and sum of a row's part
-    float* o;                           // [2 CACHE_WGS][CACHE_WG_ROWS][d]
-};
-
-template <int D, int DT, int QT>
-__global__ __launch_bounds__(256, 2) void cache_attn_kernel(sparge_cache c, CacheAttn a, const uint16_t* __restrict__ Q,
-                                                            uint16_t* __restrict__ O, Joint ws) {
-    constexpr int NK = 4 * D / 64, NV = D / 16, KS = D / 32, ROWS = 64 * QT;
-    static_assert(ROWS <= CACHE_WG_ROWS, "a part has room for that many rows");
+// Bound by the vector ALU (softmax, conversion), the matrix pipe and LDS reads about equally.  A block's codes are converted once
+// per workgroup into LDS (two buffers, one barrier per block), raw bytes two blocks ahead in registers; a wave's 32 query rows
+// share what it reads.
+template <int D, int DT>
+__global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c, CacheAttn a, Rows which, const uint16_t* __restrict__ Q,
+                                                                 uint16_t* __restrict__ O, Joint ws) {
+    constexpr int QT = WIDE_QT, NV = D / 16, KS = D / 32, RAW = D / 64;   // RAW: 16-byte pieces of K (of V) per thread
     __shared__ u64 sums[4];
-    __shared__ u64 found[2];
-    __shared__ __align__(16) float merge[3][QT][D * 16 + 32];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int G = a.H / c.H_kv;
-    const Cut cut = cut_of(G, ROWS);
+    __shared__ u64 found_rem;
+    __shared__ int found_row;
+    __shared__ __align__(16) v8h lds_k[2][4 * KS * 64], lds_v[2][NV * 2 * 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const Cut cut = cut_of(a.H / c.H_kv, WIDE_ROWS);
+    const int heads = c.H_kv * cut.parts;
 
-    // ---- this workgroup's part of the line
+    // ---- this workgroup's part of the line, in keys
     const int per = (c.R + 255) / 256;
-    u64 mine = 0;
-    for (int r = tid * per; r < min((tid + 1) * per, c.R); ++r) mine += row_info<QT>(c, a, cut, r).chunk;
-    mine *= static_cast<u64>(c.H_kv) * cut.parts;
-    u64 upto = mine;
-    for (int s = 1; s < 64; s <<= 1) {
-        const u64 x = __shfl_up(upto, s);
-        if (lane >= s) upto += x;
-    }
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    u64 total = 0;
-    for (int w = 0; w < 4; ++w) {
-        if (w < wave) upto += sums[w];
-        total += sums[w];
-    }
-    // equal parts of at least 256 weights (a block for each wave); a multiple of 8, so that neighbours on the line, which share
-    // pages, are neighbours on an XCD
-    const u64 wanted = total / 256;
-    int parts = wanted >= CACHE_WGS ? CACHE_WGS : wanted >= 8 ? static_cast<int>(wanted) & ~7 : wanted >= 1 ? static_cast<int>(wanted) : total > 0;
+    auto length_of = [&](const RowInfo& x) { return sum_vis(x, cut, a.causal, x.tiles); };
+    u64 mine = 0, total;
+    for (int r = tid * per; r < min((tid + 1) * per, c.R); ++r) mine += length_of(row_info(c, a, cut, which, r)) * heads;
+    const u64 before = prefix(mine, sums, total);
+    // equal parts of at least two blocks; a multiple of 8, so that neighbours on the line, which share pages, are neighbours on an XCD
+    const u64 wanted = total / (2 * PAGE);
+    const int parts = wanted >= WIDE_WGS ? WIDE_WGS : wanted >= 8 ? static_cast<int>(wanted) & ~7 : wanted >= 1 ? static_cast<int>(wanted) : total > 0;
     const int bid = blockIdx.x;
     if (bid >= parts) {
         if (tid == 0) ws.desc[bid].n_parts = 0;
@@ -150,407 +548,280 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(sparge_cache c, Cach
     }
     const int part = parts >= 8 ? (bid & 7) * (parts / 8) + (bid >> 3) : bid;
     const u64 lo = uniform(total * part / parts), hi = uniform(total * (part + 1) / parts);
-    if (upto - mine <= lo && lo < upto) {
-        u64 rem = lo - (upto - mine);
+    if (before <= lo && lo < before + mine) {
+        u64 rem = lo - before;
         int r = tid * per;
         for (; r < c.R - 1; ++r) {
-            const u64 all = row_info<QT>(c, a, cut, r).chunk * c.H_kv * cut.parts;
+            const u64 all = length_of(row_info(c, a, cut, which, r)) * heads;
             if (rem < all) break;
             rem -= all;
         }
-        found[0] = r;
-        found[1] = rem;
+        found_row = r;
+        found_rem = rem;
     }
     __syncthreads();
-    int r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
-    u64 rem = uniform(found[1]), pos = uniform(lo);
-    bool joins = false;
+    int r = uniform(found_row);
+    u64 rem = uniform(found_rem), pos = lo;
+    JoinDesc join = {0, 0, 0, 0, 0};
 
     while (pos < hi && r < c.R) {
-        RowInfo x = row_info<QT>(c, a, cut, r);
-        x.first = __builtin_amdgcn_readfirstlane(x.first), x.n = __builtin_amdgcn_readfirstlane(x.n);
-        x.len = __builtin_amdgcn_readfirstlane(x.len), x.p0 = __builtin_amdgcn_readfirstlane(x.p0);
-        x.tiles = __builtin_amdgcn_readfirstlane(x.tiles), x.rg = __builtin_amdgcn_readfirstlane(x.rg);
-        x.chunk = uniform(x.chunk);
-        if (rem >= x.chunk * c.H_kv * cut.parts) {
-            rem -= x.chunk * c.H_kv * cut.parts;
+        const RowInfo x = uniform(row_info(c, a, cut, which, r));
+        const u64 chunk = length_of(x);
+        if (rem >= chunk * heads) {
+            rem -= chunk * heads;
             ++r;
             continue;
         }
-        const int head = static_cast<int>(rem / x.chunk);   // kv head and part of its group
-        const u64 in = rem - head * x.chunk;
+        const int head = static_cast<int>(rem / chunk);   // kv head and part of its group
+        const u64 in = rem - head * chunk;
         int i = 0;
         for (int up = x.tiles; up - i > 1;) {
             const int mid = (i + up) >> 1;
-            if (x.rg * sum_vis(x, cut, a.causal, mid) <= in) i = mid; else up = mid;
+            if (sum_vis(x, cut, a.causal, mid) <= in) i = mid; else up = mid;
         }
-        const u64 x0 = in - x.rg * sum_vis(x, cut, a.causal, i);
+        const int x0 = static_cast<int>(in - sum_vis(x, cut, a.causal, i));
         const int ntok = min(cut.TT, x.n - i * cut.TT);
         const int vis = a.causal ? x.p0 + i * cut.TT + ntok : x.len;
-        const u64 item = static_cast<u64>(x.rg) * vis;
-        const u64 take = min(item - x0, hi - pos), x1 = x0 + take;
-        const int b0 = static_cast<int>(x0 / x.rg) / PAGE;
-        const int b1 = x1 == item ? (vis + PAGE - 1) / PAGE : static_cast<int>(x1 / x.rg) / PAGE;
-        const bool whole = x0 == 0 && x1 == item;
-        if (pos == lo && x0 > 0) {
-            // a boundary inside an item; the item's first one has it joined
-            const u64 start = lo - x0, end = start + item;
-            const bool is_first = total * (part - 1) / parts <= start;
-            joins = is_first;
-            if (tid == 0 && is_first) {
-                const u64 last = (end * parts + total - 1) / total - 1;   // the last boundary before the item's end
-                ws.desc[bid] = {static_cast<int>(last) - part + 2, part, r, head, i};
-            }
-        }
+        const int take = static_cast<int>(min(static_cast<u64>(vis - x0), hi - pos)), x1 = x0 + take;
+        const int b0 = x0 / PAGE, b1 = x1 == vis ? (vis + PAGE - 1) / PAGE : x1 / PAGE;
+        const bool whole = x0 == 0 && x1 == vis;
+        if (pos == lo && x0 > 0) join = boundary(total, parts, part, lo - x0, lo - x0 + vis, r, head, i);
 
-        // ---- one item's blocks [b0, b1)
         const int kh = head / cut.parts, gpart = head - kh * cut.parts;
-        const int rg = x.rg, kg = 4 / rg, my_rg = wave & (rg - 1), my_kg = wave / rg;
-        const int n_rows = ntok * cut.Gp;
-        const int row0 = my_rg * 16 * QT + (lane & 15);
+        const int n_rows = ntok * cut.Gp, row0 = wave * 16 * QT + (lane & 15);
         int limit[QT];
-        long long q_at[QT];
         bool valid[QT];
-        int lim_lo = 0x7FFFFFFF, lim_hi = -1;
+        uint4 q_raw[QT][KS];
+        // the wave's rows: the least and the largest key that one of them sees last
+        const int w0 = wave * 16 * QT, w1 = min(w0 + 16 * QT, n_rows) - 1;
+        const int tok_lo = w0 / cut.Gp, tok_hi = max(w1, 0) / cut.Gp;
+        const int lim_lo = a.causal ? min(x.p0 + i * cut.TT + tok_lo, x.len - 1) : x.len - 1;
+        const int lim_hi = w1 < w0 ? -1 : a.causal ? min(x.p0 + i * cut.TT + tok_hi, x.len - 1) : x.len - 1;
+        Blocks blocks;
+        blocks.open(c, a, r, kh, b0, min(b1, (x.len + PAGE - 1) / PAGE));
+        long long out_at[QT];
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
-            const int row = row0 + 16 * q, tok = row / cut.Gp, g = gpart * ROWS + row - tok * cut.Gp;
-            valid[q] = row < n_rows && g < G;
-            limit[q] = !valid[q] ? -1 : a.causal ? min(x.p0 + i * cut.TT + tok, x.len - 1) : x.len - 1;
-            q_at[q] = static_cast<long long>(x.first + i * cut.TT + tok);
-            if (valid[q]) lim_lo = min(lim_lo, limit[q]);
-            lim_hi = max(lim_hi, limit[q]);
+            const int row = row0 + 16 * q, tok = row / cut.Gp, g = gpart * WIDE_ROWS + row - tok * cut.Gp;
+            valid[q] = row < n_rows && g < cut.G;
+            limit[q] = (!valid[q] ? -1 : a.causal ? min(x.p0 + i * cut.TT + tok, x.len - 1) : x.len - 1) - 4 * (lane >> 4);
+            const long long token = x.first + i * cut.TT + tok, hd = kh * cut.G + g;
+            out_at[q] = token * a.o_sn + hd * a.o_sh;
+            load_q<D>(q_raw[q], Q + token * a.q_sn + hd * a.q_sh + 16 * (lane >> 4), valid[q]);
         }
-        for (int s = 1; s < 16; s <<= 1) {
-            lim_lo = min(lim_lo, __shfl_xor(lim_lo, s));
-            lim_hi = max(lim_hi, __shfl_xor(lim_hi, s));
-        }
-        lim_lo = __builtin_amdgcn_readfirstlane(lim_lo);
-        lim_hi = __builtin_amdgcn_readfirstlane(lim_hi);
 
-        // Q: fp16 as it is; bf16 times the power of two that brings the row's largest to [1, 2) (exact but for what is below
-        // 2^-24 of it).  An operand holds, of channels 64 s + 16 (lane / 16) + 8 u + 0..7, the one of step 2 s + u.
+        uint4 kraw[RAW], vraw[RAW];
+        auto load_raw = [&](int page) {
+            const long long at = (static_cast<long long>(page) * c.H_kv + kh) * (PAGE * D) + tid * 16;
+#pragma unroll
+            for (int n = 0; n < RAW; ++n) {
+                kraw[n] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(c.k) + at + n * 4096);
+                vraw[n] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(c.v) + at + n * 4096);
+            }
+        };
+        auto convert = [&](int buf) {   // piece p = tid + 256 n of 64 lanes each: operands 2 (p / 64) and 2 (p / 64) + 1
+#pragma unroll
+            for (int n = 0; n < RAW; ++n) {
+                const int op = 2 * (wave + 4 * n);
+                lds_k[buf][op * 64 + lane] = codes8(kraw[n].x, kraw[n].y);
+                lds_k[buf][(op + 1) * 64 + lane] = codes8(kraw[n].z, kraw[n].w);
+                lds_v[buf][op * 64 + lane] = codes8(vraw[n].x, vraw[n].y);
+                lds_v[buf][(op + 1) * 64 + lane] = codes8(vraw[n].z, vraw[n].w);
+            }
+        };
+        int block = 0, page = 0, at = 0, n_block = 0, n_at = 0;
+        float ka = 0.f, va = 0.f, n_ka = 0.f, n_va = 0.f;
+        bool more = blocks.next(c, kh, block, page, at), n_more = false;
+        if (more) {
+            load_raw(page);
+            ka = blocks.ka(at), va = blocks.va(at);
+        }
         v8h qf[QT][KS];
-        float qs[QT];
-#pragma unroll
-        for (int q = 0; q < QT; ++q) {
-            const int row = row0 + 16 * q, tok = row / cut.Gp, g = gpart * ROWS + row - tok * cut.Gp;
-            uint4 raw[KS];
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                raw[s] = make_uint4(0u, 0u, 0u, 0u);
-                if (valid[q])
-                    raw[s] = *reinterpret_cast<const uint4*>(Q + q_at[q] * a.q_sn + static_cast<long long>(kh * G + g) * a.q_sh +
-                                                             64 * (s >> 1) + 16 * (lane >> 4) + 8 * (s & 1));
-            }
-            qs[q] = a.scale_log2;
-            if constexpr (DT == SPARGE_F16) {
-#pragma unroll
-                for (int s = 0; s < KS; ++s) __builtin_memcpy(&qf[q][s], &raw[s], 16);
-            } else {
-                uint32_t top = 0;
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7FFFu, (w[e] >> 16) & 0x7FFFu));
-                }
-                top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 16)));
-                top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32)));
-                int ex = static_cast<int>(top >> 7) - 127;          // exponent of the largest (top: bf16 bits)
-                if (ex > 127 || top == 0) ex = 0;                   // NaN and infinity stay what they are
-                const float down = ldexpf(1.0f, -ex);
-                qs[q] *= ldexpf(1.0f, ex);
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        qf[q][s][2 * e] = static_cast<_Float16>(cvt16<DT>(static_cast<uint16_t>(w[e] & 0xFFFFu)) * down);
-                        qf[q][s][2 * e + 1] = static_cast<_Float16>(cvt16<DT>(static_cast<uint16_t>(w[e] >> 16)) * down);
-                    }
-                }
-            }
-        }
-
+        float qs[QT], m[QT], l[QT];
         v4f o[QT][NV];
-        float m[QT], l[QT];
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
+            qs[q] = a.scale_log2 * convert_q<D, DT>(q_raw[q], qf[q]);
             m[q] = FAR, l[q] = 0.f;
 #pragma unroll
             for (int n = 0; n < NV; ++n) o[q][n] = {0.f, 0.f, 0.f, 0.f};
         }
-        float sv_ref = 0.f;
-
-        // blocks: 64 table entries at a time, one a lane; of the kept ones a wave takes those of its rank
-        int base = b0 - 64, seen_blocks = 0;
-        const int end = lim_hi < 0 ? 0 : min(b1, lim_hi / PAGE + 1);
-        u64 bits = 0;
-        int l_page = 0;
-        float l_ka = 0.f, l_va = 0.f;
-        const long long table_at = static_cast<long long>(r) * c.max_blocks;
-        const long long mask_at = (static_cast<long long>(r) * c.H_kv + kh) * c.max_blocks;
-        auto next = [&](int& block, int& page, float& ka, float& va) -> bool {
-            while (bits == 0) {
-                base += 64;
-                if (base >= end) return false;
-                const int j = base + lane;
-                bool keep = j < end;
-                l_page = -1;
-                if (keep) {
-                    l_page = c.table[table_at + j];
-                    keep = l_page >= 0 && l_page < c.n_pages && (!a.mask || a.mask[mask_at + j]);
-                }
-                if (keep) {
-                    l_ka = c.k_amax[static_cast<long long>(l_page) * c.H_kv + kh];
-                    l_va = c.v_amax[static_cast<long long>(l_page) * c.H_kv + kh];
-                }
-                const u64 kept = __ballot(keep);
-                const int rank = seen_blocks + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(kept >> 32),
-                                                                          __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(kept), 0));
-                bits = __ballot(keep && (rank & (kg - 1)) == my_kg);
-                seen_blocks += __builtin_popcountll(kept);
-            }
-            const int b = __builtin_ctzll(bits);
-            bits &= bits - 1;
-            block = base + b;
-            page = __builtin_amdgcn_readlane(l_page, b);
-            ka = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l_ka), b));
-            va = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l_va), b));
-            return true;
-        };
-        uint4 kraw[NK], vraw[NV];
-        auto load_k = [&](int page) {
-            const uint8_t* p = static_cast<const uint8_t*>(c.k) + (static_cast<long long>(page) * c.H_kv + kh) * (PAGE * D) + lane * 16;
-#pragma unroll
-            for (int n = 0; n < NK; ++n) kraw[n] = *reinterpret_cast<const uint4*>(p + n * 1024);
-        };
-        auto load_v = [&](int page) {
-            const uint8_t* p = static_cast<const uint8_t*>(c.v) + (static_cast<long long>(page) * c.H_kv + kh) * (PAGE * D) + lane * 16;
-#pragma unroll
-            for (int n = 0; n < NV; ++n) vraw[n] = *reinterpret_cast<const uint4*>(p + n * 1024);
-        };
-        int block, page;
-        float ka, va;
-        bool more = next(block, page, ka, va);
+        VScale vs;
         if (more) {
-            load_k(page);
-            load_v(page);
+            convert(0);
+            n_more = blocks.next(c, kh, n_block, page, n_at);
+            if (n_more) {
+                load_raw(page);
+                n_ka = blocks.ka(n_at), n_va = blocks.va(n_at);
+            }
         }
-        while (more) {
-            v4f s[QT][4];
+        __syncthreads();
+        for (int buf = 0; more; buf ^= 1) {
+            // the next block's bytes into the other buffer, the one after it on its way
+            int nn_block = 0, nn_at = 0;
+            float nn_ka = 0.f, nn_va = 0.f;
+            bool nn_more = false;
+            if (n_more) {
+                convert(buf ^ 1);
+                nn_more = blocks.next(c, kh, nn_block, page, nn_at);
+                if (nn_more) {
+                    load_raw(page);
+                    nn_ka = blocks.ka(nn_at), nn_va = blocks.va(nn_at);
+                }
+            }
+            if (block * PAGE <= lim_hi) {
+                v4f s[QT][4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
+                for (int t = 0; t < 4; ++t) {
 #pragma unroll
-                for (int q = 0; q < QT; ++q) s[q][t] = {0.f, 0.f, 0.f, 0.f};
+                    for (int q = 0; q < QT; ++q) s[q][t] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int e = 0; e < D / 64; ++e) {
-                    const uint4 w = kraw[t * (D / 64) + e];
-                    const v8h k0 = codes8(w.x, w.y), k1 = codes8(w.z, w.w);
+                    for (int e = 0; e < KS; ++e) {
+                        const v8h k = lds_k[buf][(t * KS + e) * 64 + lane];
+#pragma unroll
+                        for (int q = 0; q < QT; ++q) s[q][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[q][e], s[q][t], 0, 0, 0);
+                    }
+                }
+                const float down = vs.take(va);
+                if (down != 1.0f) {
+#pragma unroll
+                    for (int q = 0; q < QT; ++q)
+#pragma unroll
+                        for (int n = 0; n < NV; ++n) o[q][n] *= down;
+                }
+                const bool masked = block * PAGE + PAGE - 1 > lim_lo;
+                const float sk = ka * (1.0f / 127.0f);
+                v8h pf[QT][2];
+#pragma unroll
+                for (int q = 0; q < QT; ++q) softmax<NV>(s[q], qs[q] * sk, vs, masked, limit[q] - block * PAGE, m[q], l[q], o[q], pf[q]);
+#pragma unroll
+                for (int n = 0; n < NV; ++n) {
+                    const v8h v0 = lds_v[buf][2 * n * 64 + lane], v1 = lds_v[buf][(2 * n + 1) * 64 + lane];
 #pragma unroll
                     for (int q = 0; q < QT; ++q) {
-                        s[q][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf[q][2 * e], s[q][t], 0, 0, 0);
-                        s[q][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[q][2 * e + 1], s[q][t], 0, 0, 0);
+                        o[q][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[q][0], o[q][n], 0, 0, 0);
+                        o[q][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[q][1], o[q][n], 0, 0, 0);
                     }
                 }
             }
-            int n_block = 0, n_page = 0;
-            float n_ka = 0.f, n_va = 0.f;
-            const bool n_more = next(n_block, n_page, n_ka, n_va);
-            if (n_more) load_k(n_page);
-
-            const bool masked = block * PAGE + PAGE - 1 > lim_lo;
-            const float sk = ka * (1.0f / 127.0f);
-            if (va > SV_SLACK * sv_ref && va < INFINITY) {
-                const float down = sv_ref / va;
-#pragma unroll
-                for (int q = 0; q < QT; ++q)
-#pragma unroll
-                    for (int n = 0; n < NV; ++n) o[q][n] *= down;
-                sv_ref = va;
-            }
-            const float f = P_UP * (sv_ref > 0.f ? va / sv_ref : va);
-            v8h pf[QT][2];
-#pragma unroll
-            for (int q = 0; q < QT; ++q) {
-                float cq = qs[q] * sk;
-                if (cq == 0.f) cq = 1e-37f;   // a block of zeros: -inf below stays what it is
-                float top = -INFINITY;
-                if (masked) {
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (block * PAGE + 16 * t + 4 * (lane >> 4) + e > limit[q]) s[q][t][e] = -INFINITY;
-                }
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) top = fmaxf(top, s[q][t][e]);
-                top = max_groups(top) * cq;
-                if (__any(top > m[q] + SLACK)) {
-                    const float to = fmaxf(m[q], top), down = __builtin_amdgcn_exp2f(m[q] - to);
-                    m[q] = to;
-                    l[q] *= down;
-#pragma unroll
-                    for (int n = 0; n < NV; ++n) o[q][n] *= down;
-                }
-                float p[16];
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) p[4 * t + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][t][e], cq, -m[q]));
-                float w[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) w[e] = p[e] * f;
-                if (masked) {   // a key that is not seen has no weight even where the block's scales are NaN or infinite
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (block * PAGE + 16 * t + 4 * (lane >> 4) + e > limit[q]) p[4 * t + e] = w[4 * t + e] = 0.f;
-                }
-                float sum = 0.f;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) sum += p[e];
-                l[q] += sum;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) pf[q][e >> 3][e & 7] = static_cast<_Float16>(w[e]);
-            }
-#pragma unroll
-            for (int n = 0; n < NV; ++n) {
-                const v8h v0 = codes8(vraw[n].x, vraw[n].y), v1 = codes8(vraw[n].z, vraw[n].w);
-#pragma unroll
-                for (int q = 0; q < QT; ++q) {
-                    o[q][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[q][0], o[q][n], 0, 0, 0);
-                    o[q][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[q][1], o[q][n], 0, 0, 0);
-                }
-            }
-            if (n_more) load_v(n_page);
-            more = n_more, block = n_block, page = n_page, ka = n_ka, va = n_va;
+            __syncthreads();
+            more = n_more, block = n_block, ka = n_ka, va = n_va;
+            n_more = nn_more, n_block = nn_block, n_ka = nn_ka, n_va = nn_va;
         }
 
-        // ---- the waves that shared rows are joined, then the rows are written, whole or as a part
-        const float o_scale = sv_ref * (1.0f / (127.0f * P_UP));
+        const float o_scale = vs.ref * (1.0f / (127.0f * 256.0f));
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
             l[q] = sum_groups(l[q]);
-#pragma unroll
-            for (int n = 0; n < NV; ++n) o[q][n] *= o_scale;
-        }
-        if (kg > 1) {
-            if (my_kg > 0) {
-#pragma unroll
-                for (int q = 0; q < QT; ++q) {
-                    float* at = merge[wave - rg][q];
-#pragma unroll
-                    for (int n = 0; n < NV; ++n) reinterpret_cast<v4f*>(at)[n * 64 + lane] = o[q][n];
-                    if (lane < 16) at[D * 16 + lane] = m[q], at[D * 16 + 16 + lane] = l[q];
-                }
-            }
-            __syncthreads();
-            if (my_kg == 0) {
-#pragma unroll
-                for (int q = 0; q < QT; ++q)
-                    for (int k = 1; k < kg; ++k) {
-                        const float* at = merge[k * rg + my_rg - rg][q];
-                        const float om = at[D * 16 + (lane & 15)], ol = at[D * 16 + 16 + (lane & 15)];
-                        const float to = fmaxf(m[q], om);
-                        const float wa = __builtin_amdgcn_exp2f(m[q] - to), wb = __builtin_amdgcn_exp2f(om - to);
-                        m[q] = to;
-                        l[q] = l[q] * wa + ol * wb;
-#pragma unroll
-                        for (int n = 0; n < NV; ++n) o[q][n] = o[q][n] * wa + reinterpret_cast<const v4f*>(at)[n * 64 + lane] * wb;
-                    }
-            }
-            __syncthreads();
-        }
-        if (my_kg == 0) {
-            const int slot = 2 * part + (x0 > 0 ? 0 : 1);
-#pragma unroll
-            for (int q = 0; q < QT; ++q) {
-                if (!valid[q]) continue;
-                const int row = row0 + 16 * q, tok = row / cut.Gp, g = gpart * ROWS + row - tok * cut.Gp;
-                if (whole) {
-                    const float inv = l[q] == 0.f ? 0.f : 1.0f / l[q];
-                    uint16_t* out = O + q_at[q] * a.o_sn + static_cast<long long>(kh * G + g) * a.o_sh + 4 * (lane >> 4);
-#pragma unroll
-                    for (int n = 0; n < NV; ++n) {
-                        uint2 w;
-                        uint16_t h[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) h[e] = l[q] == 0.f ? 0 : cvt_to16<DT>(o[q][n][e] * inv);
-                        __builtin_memcpy(&w, h, 8);
-                        *reinterpret_cast<uint2*>(out + 16 * n) = w;
-                    }
-                } else {
-                    const long long at = static_cast<long long>(slot) * CACHE_WG_ROWS + row;
-#pragma unroll
-                    for (int n = 0; n < NV; ++n)
-                        *reinterpret_cast<v4f*>(ws.o + at * D + 16 * n + 4 * (lane >> 4)) = o[q][n];
-                    if (lane < 16) ws.ml[2 * at] = m[q], ws.ml[2 * at + 1] = l[q];
-                }
-            }
+            if (!valid[q]) continue;
+            if (whole) store_whole<NV, DT>(o[q], l[q], o_scale, O + out_at[q] + 4 * (lane >> 4));
+            else store_part<NV>(o[q], m[q], l[q], o_scale, ws, static_cast<long long>(2 * part + (x0 > 0 ? 0 : 1)) * WIDE_ROWS + row0 + 16 * q);
         }
         pos += take;
         rem += take;
     }
-    if (tid == 0 && !joins) ws.desc[bid].n_parts = 0;
+    if (tid == 0) ws.desc[bid] = join;
 }
 
-// Joins an item that several workgroups have parts of, in their order.
-template <int D, int DT, int QT>
-__global__ __launch_bounds__(256) void cache_join_kernel(sparge_cache c, CacheAttn a, uint16_t* __restrict__ O, Joint ws) {
-    constexpr int ROWS = 64 * QT, TPR = D / 4;   // threads per row, 4 channels each
-    const JoinDesc d = ws.desc[blockIdx.x];
-    if (d.n_parts == 0) return;
-    const int G = a.H / c.H_kv;
-    const Cut cut = cut_of(G, ROWS);
-    const RowInfo x = row_info<QT>(c, a, cut, d.row);
-    const int kh = d.head / cut.parts, gpart = d.head - kh * cut.parts;
-    const int n_rows = min(cut.TT, x.n - d.tile * cut.TT) * cut.Gp, ch = (threadIdx.x % TPR) * 4;
-    // the item's start is the second part of the workgroup before the first boundary, the rest first parts
-    auto slot = [&](int k) { return static_cast<long long>(k == 0 ? 2 * (d.part - 1) + 1 : 2 * (d.part + k - 1)) * CACHE_WG_ROWS; };
-    for (int row = threadIdx.x / TPR; row < n_rows; row += 256 / TPR) {
-        const int tok = row / cut.Gp, g = gpart * ROWS + row - tok * cut.Gp;
-        if (g >= G) continue;
-        float m = FAR, l = 0.f;
-        for (int k = 0; k < d.n_parts; ++k) m = fmaxf(m, ws.ml[2 * (slot(k) + row)]);
-        v4f o = {0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < d.n_parts; ++k) {
-            const long long at = slot(k) + row;
-            const float w = __builtin_amdgcn_exp2f(ws.ml[2 * at] - m);
-            l += ws.ml[2 * at + 1] * w;
-            o += *reinterpret_cast<const v4f*>(ws.o + at * D + ch) * w;
-        }
-        uint16_t h[4];
+// ---- join ----------------------------------------------------------------------------------------------------------
+
+// Joins an item that several parts hold, in their order: workgroup x looks at `descs` parts that might be the first one to
+// begin inside an item, and takes every JOIN_Y-th row.  A row's channels take D / 4 threads, its parts are dealt out over
+// the 1024 / D groups of that many, whose results go through LDS; where there are few parts the groups take rows instead.
+template <int D, int DT, int ROWS>
+__global__ __launch_bounds__(256) void cache_join_kernel(sparge_cache c, CacheAttn a, Rows which, int descs, uint16_t* __restrict__ O, Joint ws) {
+    constexpr int TPR = D / 4, GROUPS = 256 / TPR;   // threads per row, groups of them
+    __shared__ __align__(16) v4f lds_o[GROUPS][TPR];
+    __shared__ float lds_m[GROUPS], lds_l[GROUPS];
+    const int grp = threadIdx.x / TPR, ch = (threadIdx.x % TPR) * 4;
+    const Cut cut = cut_of(a.H / c.H_kv, ROWS);
+    for (int n = 0; n < descs; ++n) {
+        const JoinDesc d = ws.desc[blockIdx.x * descs + n];
+        if (d.n_parts == 0) continue;
+        const RowInfo x = row_info(c, a, cut, which, d.row);
+        const int kh = d.head / cut.parts, gpart = d.head - kh * cut.parts;
+        const int n_rows = min(cut.TT, x.n - d.tile * cut.TT) * cut.Gp;
+        // the item's start is the second result of the part before the first boundary, the rest are first results
+        auto slot = [&](int k) { return static_cast<long long>(k == 0 ? 2 * (d.part - 1) + 1 : 2 * (d.part + k - 1)) * ROWS; };
+        const bool deal = d.n_parts > 4;
+        const int k0 = deal ? grp : 0, ks = deal ? GROUPS : 1;
+        for (int base = 0; base < n_rows; base += deal ? JOIN_Y : JOIN_Y * GROUPS) {
+            const int row = base + (deal ? static_cast<int>(blockIdx.y) : static_cast<int>(blockIdx.y) * GROUPS + grp);
+            const int tok = row / cut.Gp, g = gpart * ROWS + row - tok * cut.Gp;
+            const bool there = row < n_rows && g < cut.G;
+            float m = FAR, l = 0.f;
+            v4f o = {0.f, 0.f, 0.f, 0.f};
+            if (there) {
+                float top = FAR;
+#pragma unroll 4
+                for (int k = k0; k < d.n_parts; k += ks) top = fmaxf(top, ws.ml[2 * (slot(k) + row)]);
+                m = top;
+#pragma unroll 4
+                for (int k = k0; k < d.n_parts; k += ks) {
+                    const long long at = slot(k) + row;
+                    const float w = __builtin_amdgcn_exp2f(ws.ml[2 * at] - m);
+                    l += ws.ml[2 * at + 1] * w;
+                    o += *reinterpret_cast<const v4f*>(ws.o + at * D + ch) * w;
+                }
+            }
+            if (deal) {
+                __syncthreads();
+                lds_o[grp][ch / 4] = o;
+                if (ch == 0) lds_m[grp] = m, lds_l[grp] = l;
+                __syncthreads();
+                if (grp == 0) {
+                    for (int k = 1; k < GROUPS; ++k) m = fmaxf(m, lds_m[k]);
+                    l = 0.f, o = {0.f, 0.f, 0.f, 0.f};
+                    for (int k = 0; k < GROUPS; ++k) {
+                        const float w = __builtin_amdgcn_exp2f(lds_m[k] - m);
+                        l += lds_l[k] * w;
+                        o += lds_o[k][ch / 4] * w;
+                    }
+                }
+            }
+            if (there && (!deal || grp == 0)) {
+                uint16_t h[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = l == 0.f ? 0 : cvt_to16<DT>(o[e] / l);
-        uint2 w;
-        __builtin_memcpy(&w, h, 8);
-        *reinterpret_cast<uint2*>(O + static_cast<long long>(x.first + d.tile * cut.TT + tok) * a.o_sn +
-                                  static_cast<long long>(kh * G + g) * a.o_sh + ch) = w;
+                for (int e = 0; e < 4; ++e) h[e] = l == 0.f ? 0 : cvt_to16<DT>(o[e] / l);
+                uint2 w;
+                __builtin_memcpy(&w, h, 8);
+                *reinterpret_cast<uint2*>(O + static_cast<long long>(x.first + d.tile * cut.TT + tok) * a.o_sn +
+                                          static_cast<long long>(kh * cut.G + g) * a.o_sh + ch) = w;
+            }
+        }
     }
 }
 
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+// The workspace: descriptions, references and sums, partial rows.  The two kernels use the same room one after the other.
+constexpr size_t MOST_ROWS = 2ull * (NARROW_PARTS * NARROW_ROWS > WIDE_WGS * WIDE_ROWS ? NARROW_PARTS * NARROW_ROWS : WIDE_WGS * WIDE_ROWS);
 struct Layout {
     size_t ml, o, total;
 };
 Layout layout_of(int d) {
-    const size_t up = 255, rows = 2ull * CACHE_WGS * CACHE_WG_ROWS;
+    const size_t up = 255;
     Layout x;
-    x.ml = (CACHE_WGS * sizeof(JoinDesc) + up) & ~up;
-    x.o = x.ml + rows * 2 * sizeof(float);
-    x.total = x.o + rows * d * sizeof(float);
+    x.ml = (NARROW_PARTS * sizeof(JoinDesc) + up) & ~up;
+    x.o = x.ml + MOST_ROWS * 2 * sizeof(float);
+    x.total = x.o + MOST_ROWS * d * sizeof(float);
     return x;
 }
 
-template <int D, int DT, int QT>
-void launch(const sparge_cache& c, const CacheAttn& a, const void* Q, void* O, const Joint& j, hipStream_t st) {
-    hipLaunchKernelGGL((cache_attn_kernel<D, DT, QT>), dim3(CACHE_WGS), dim3(256), 0, st, c, a, static_cast<const uint16_t*>(Q),
-                       static_cast<uint16_t*>(O), j);
-    hipLaunchKernelGGL((cache_join_kernel<D, DT, QT>), dim3(CACHE_WGS), dim3(256), 0, st, c, a, static_cast<uint16_t*>(O), j);
+template <int D, int DT>
+void launch(const sparge_cache& c, const CacheAttn& a, bool narrow, bool wide, const void* Qp, void* Op, const Joint& j, hipStream_t st) {
+    const uint16_t* Q = static_cast<const uint16_t*>(Qp);
+    uint16_t* O = static_cast<uint16_t*>(Op);
+    if (narrow) {
+        const Rows which = wide ? FEW_ROWS : ALL_ROWS;
+        hipLaunchKernelGGL((cache_attn_narrow_kernel<D, DT>), dim3(NARROW_WGS), dim3(256), 0, st, c, a, which, Q, O, j);
+        hipLaunchKernelGGL((cache_join_kernel<D, DT, NARROW_ROWS>), dim3(NARROW_WGS, JOIN_Y), dim3(256), 0, st, c, a, which, 4, O, j);
+    }
+    if (wide) {
+        const Rows which = narrow ? MANY_ROWS : ALL_ROWS;
+        hipLaunchKernelGGL((cache_attn_wide_kernel<D, DT>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, which, Q, O, j);
+        hipLaunchKernelGGL((cache_join_kernel<D, DT, WIDE_ROWS>), dim3(WIDE_WGS, JOIN_Y), dim3(256), 0, st, c, a, which, 1, O, j);
+    }
 }
 
 }  // namespace
@@ -561,9 +832,13 @@ hipError_t launch_cache_attn(const sparge_cache& c, const CacheAttn& a, const vo
     const Layout x = layout_of(c.d);
     char* p = static_cast<char*>(ws);
     const Joint j = {reinterpret_cast<JoinDesc*>(p), reinterpret_cast<float*>(p + x.ml), reinterpret_cast<float*>(p + x.o)};
-    // two tiles of 16 rows a wave where the rows of the cache have more query rows on average than four waves' single ones
-    const bool wide = static_cast<long long>(a.n_slots) * (a.H / c.H_kv) > 64ll * c.R;
-#define RUN(D, DT) wide ? launch<D, DT, 2>(c, a, Q, O, j, st) : launch<D, DT, 1>(c, a, Q, O, j, st)
+    // How many tokens each row adds is not known here.  With no more tokens than rows, one each is the case to be fast in, whose
+    // group fits a wave or does not; with a single row it is known; else both kernels run, each on its rows.
+    const int G = a.H / c.H_kv;
+    const bool one_kind = a.n_slots <= c.R || c.R == 1;
+    const bool few = static_cast<long long>(c.R == 1 ? a.n_slots : 1) * G <= NARROW_ROWS;
+    const bool narrow = one_kind ? few : G <= NARROW_ROWS, wide = one_kind ? !few : true;
+#define RUN(D, DT) launch<D, DT>(c, a, narrow, wide, Q, O, j, st)
     if (c.d == 64) {
         if (c.dtype == SPARGE_F16) RUN(64, SPARGE_F16); else RUN(64, SPARGE_BF16);
     } else {
