@@ -30,9 +30,12 @@ struct CacheAttn {
 
 // What the joining launch has to know of a part of the attention's work.
 struct JoinDesc {
-    int n_parts;                        // 0: nothing to join here
-    int part, row, head, tile;          // the part whose beginning is the first boundary inside the item; the item
+    int n_parts;                        // that the item has; 0: nothing to join here
+    int first, part;                    // the first part that begins inside the item; this one
+    int token, n_tok, head, n_heads;    // the item's rows of Q and O
+    int pad;                            // (two 16-byte loads)
 };
+constexpr JoinDesc NO_JOIN = {0, 0, 0, 0, 0, 0, 0, 0};
 size_t cache_attn_workspace(int d);
 
 hipError_t launch_cache_plan(const sparge_cache& c, const int32_t* new_len, const uint8_t* release, int n_slots, int32_t* cu,

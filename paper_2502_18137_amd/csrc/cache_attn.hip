@@ -33,8 +33,7 @@ constexpr float P_UP_LOG2 = 8.0f;      // p is at most 2^4, its factor sv ratio 
 constexpr float SV_LEAST = 0x1p-60f;   // smaller ratios (and blocks of zeros) count as this: below every rounding beside sv_ref
 
 constexpr int NARROW_ROWS = 16, NARROW_WGS = 512, NARROW_PARTS = 4 * NARROW_WGS;   // two workgroups per compute unit
-constexpr int WIDE_QT = 2, WIDE_ROWS = 64 * WIDE_QT, WIDE_WGS = 512;
-constexpr int JOIN_Y = 4;              // workgroups among which an item's rows are dealt out
+constexpr int WIDE_ROWS = 128, WIDE_WGS = 512;
 
 template <int X>
 __device__ __forceinline__ float other(float v) {   // of lane ^ X, X = 16 or 32
@@ -132,11 +131,12 @@ __device__ __forceinline__ u64 prefix(u64 v, u64* lds, u64& total) {
     return upto - v;
 }
 
-// Where a part begins inside an item: what the join needs.  start, end: the item on the line.
-__device__ __forceinline__ JoinDesc boundary(u64 total, int parts, int part, u64 start, u64 end, int row, int head, int tile) {
-    if (total * (part - 1) / parts > start) return {0, 0, 0, 0, 0};          // not the item's first boundary
-    const u64 last = (end * parts + total - 1) / total - 1;                   // its last one
-    return {static_cast<int>(last) - part + 2, part, row, head, tile};
+// A part that begins inside an item: what the join needs.  start, end: the item on the line; token, head: its first.
+__device__ __forceinline__ JoinDesc boundary(u64 total, int parts, int part, u64 start, u64 end, int token, int n_tok, int head, int n_heads) {
+    int first = static_cast<int>(start * parts / total);                      // the first part that begins inside it
+    while (total * first / parts <= start) ++first;
+    const u64 last = (end * parts + total - 1) / total - 1;
+    return {static_cast<int>(last) - first + 2, first, part, token, n_tok, head, n_heads, 0};
 }
 
 // The blocks of an item's range, 64 table entries at a time, one a lane, the next 64 on their way.
@@ -191,6 +191,28 @@ __device__ __forceinline__ void load_q(uint4 (&raw)[D / 32], const uint16_t* row
         if (valid) raw[s] = *reinterpret_cast<const uint4*>(row + 64 * (s >> 1) + 8 * (s & 1));
     }
 }
+__device__ __forceinline__ uint32_t top16(const uint4& raw) {   // the largest |x| of 8 bf16, as its bits
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7FFFu, (w[e] >> 16) & 0x7FFFu));
+    return top;
+}
+__device__ __forceinline__ int exponent16(uint32_t top) {       // of bf16 bits; 0 for zero, infinity and NaN, which stay what they are
+    const int ex = static_cast<int>(top >> 7) - 127;
+    return ex > 127 || top == 0 ? 0 : ex;
+}
+template <int DT>
+__device__ __forceinline__ v8h scaled8(const uint4& raw, float by) {
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    v8h r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        r[2 * e] = static_cast<_Float16>(cvt16<DT>(static_cast<uint16_t>(w[e] & 0xFFFFu)) * by);
+        r[2 * e + 1] = static_cast<_Float16>(cvt16<DT>(static_cast<uint16_t>(w[e] >> 16)) * by);
+    }
+    return r;
+}
 template <int D, int DT>
 __device__ __forceinline__ float convert_q(const uint4 (&raw)[D / 32], v8h (&qf)[D / 32]) {
     if constexpr (DT == SPARGE_F16) {
@@ -200,28 +222,21 @@ __device__ __forceinline__ float convert_q(const uint4 (&raw)[D / 32], v8h (&qf)
     } else {
         uint32_t top = 0;
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7FFFu, (w[e] >> 16) & 0x7FFFu));
-        }
+        for (int s = 0; s < D / 32; ++s) top = max(top, top16(raw[s]));
         top = max(top, __float_as_uint(other<16>(__uint_as_float(top))));
         top = max(top, __float_as_uint(other<32>(__uint_as_float(top))));
-        int ex = static_cast<int>(top >> 7) - 127;          // exponent of the largest (top: bf16 bits)
-        if (ex > 127 || top == 0) ex = 0;                   // NaN and infinity stay what they are
+        const int ex = exponent16(top);
         const float down = __builtin_ldexpf(1.0f, -ex);
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                qf[s][2 * e] = static_cast<_Float16>(cvt16<DT>(static_cast<uint16_t>(w[e] & 0xFFFFu)) * down);
-                qf[s][2 * e + 1] = static_cast<_Float16>(cvt16<DT>(static_cast<uint16_t>(w[e] >> 16)) * down);
-            }
-        }
+        for (int s = 0; s < D / 32; ++s) qf[s] = scaled8<DT>(raw[s], down);
         return __builtin_ldexpf(1.0f, ex);
     }
 }
+
+// A block with a NaN or an infinity in K or V: its codes are 0; the queries that see one of its keys get NaN, through their
+// sums, and the others nothing.
+__device__ __forceinline__ bool not_finite(float ka, float va) { return !(ka < INFINITY && va < INFINITY); }
+__device__ __forceinline__ float nan_f() { return __uint_as_float(0x7FC00000u); }
 
 // V's scale of a block against the one that O is relative to: the factor's log2 (with P_UP_LOG2) and inverse.
 struct VScale {
@@ -230,9 +245,9 @@ struct VScale {
     // -> what O has to be multiplied with first (1: nothing)
     __device__ __forceinline__ float take(float va) {
         float down = 1.0f;
-        if (va > SV_SLACK * ref && va < INFINITY) down = ref / va, ref = va;
-        float f = va / ref;                          // (NaN and infinity stay; 0 / 0: codes are 0)
-        if (va < SV_LEAST * ref || va == 0.f) f = SV_LEAST;
+        if (va > SV_SLACK * ref) down = ref / va, ref = va;
+        float f = va / ref;
+        if (va < SV_LEAST * ref || va == 0.f) f = SV_LEAST;   // (a block of zeros has codes 0 whatever the factor)
         f_log2 = __builtin_amdgcn_logf(f) + P_UP_LOG2, f_inv = __builtin_amdgcn_rcpf(f) * 0x1p-8f;
         return down;
     }
@@ -244,7 +259,7 @@ struct VScale {
 template <int NV>
 __device__ __forceinline__ void softmax(v4f (&s)[4], float cq, const VScale& v, bool masked, int last, float& m, float& l,
                                         v4f (&o)[NV], v8h (&pf)[2]) {
-    if (cq == 0.f) cq = 1e-37f;   // a block of zeros: -inf below stays what it is
+    if (cq == 0.f) cq = 1e-37f;   // a block of zeros: -inf stays what it is and becomes a weight of 0
     if (masked) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -271,17 +286,10 @@ __device__ __forceinline__ void softmax(v4f (&s)[4], float cq, const VScale& v, 
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[4 * t + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], cq, from));
-    if (masked) {   // a key that is not seen has no weight even where the block's scales are NaN or infinite
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (16 * t + e > last) w[4 * t + e] = 0.f;
-    }
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) sum += w[e];
-    l += masked && sum == 0.f ? 0.f : sum * v.f_inv;
+    l += sum * v.f_inv;
 #pragma unroll
     for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = static_cast<_Float16>(w[e]);
 }
@@ -320,6 +328,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache 
     __shared__ u64 sums[4];
     __shared__ u64 found_rem[4];
     __shared__ int found_row[4];
+    __shared__ RowInfo found_info[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const Cut cut = cut_of(a.H / c.H_kv, NARROW_ROWS);
     const int heads = c.H_kv * cut.parts;
@@ -339,18 +348,19 @@ __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache 
         if (before <= at && at < before + mine) {
             u64 rem = at - before;
             int r = tid * per;
-            for (; r < c.R - 1; ++r) {
-                const u64 all = length_of(row_info(c, a, cut, which, r));
-                if (rem < all) break;
-                rem -= all;
+            RowInfo x = row_info(c, a, cut, which, r);
+            for (; rem >= length_of(x) && r < c.R - 1; x = row_info(c, a, cut, which, r)) {
+                rem -= length_of(x);
+                ++r;
             }
             found_row[w] = r;
             found_rem[w] = rem;
+            found_info[w] = x;
         }
     }
     __syncthreads();
     if (part >= parts) {
-        if (lane == 0) ws.desc[part].n_parts = 0;
+        if (lane == 0) ws.desc[part] = NO_JOIN;
         return;
     }
     const u64 lo = uniform(total * part / parts);
@@ -358,6 +368,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache 
     u64 rem = uniform(found_rem[wave]);                       // where in row `r` the next ones begin
     int r = uniform(found_row[wave]);
     bool first_item = true;
+    RowInfo info = uniform(found_info[wave]);                 // row `r`
 
     struct Item {
         RowInfo x;
@@ -365,12 +376,12 @@ __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache 
     };
     auto next_item = [&](Item& it) -> bool {
         while (left > 0 && r < c.R) {
-            it.x = uniform(row_info(c, a, cut, which, r));
+            it.x = info;
             it.blocks = (it.x.len + PAGE - 1) / PAGE;
             const u64 all = length_of(it.x);
             if (rem >= all) {
                 rem -= all;
-                ++r;
+                if (++r < c.R) info = uniform(row_info(c, a, cut, which, r));
                 continue;
             }
             const uint32_t tile = static_cast<uint32_t>(rem / static_cast<uint32_t>(it.blocks));   // of all heads' tiles
@@ -382,8 +393,11 @@ __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache 
             const u64 take = min(static_cast<u64>(it.blocks - it.b0), left);
             it.b1 = it.b0 + static_cast<int>(take);
             if (first_item) {
-                JoinDesc d = {0, 0, 0, 0, 0};
-                if (it.b0 > 0) d = boundary(total, parts, part, lo - it.b0, lo - it.b0 + it.blocks, r, head, it.tile);
+                JoinDesc d = NO_JOIN;
+                const int g0 = it.gpart * NARROW_ROWS;
+                if (it.b0 > 0)
+                    d = boundary(total, parts, part, lo - it.b0, lo - it.b0 + it.blocks, it.x.first + it.tile * cut.TT, it.ntok,
+                                 it.kh * cut.G + g0, min(cut.Gp, cut.G - g0));
                 if (lane == 0) ws.desc[part] = d;
                 first_item = false;
             }
@@ -424,7 +438,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache 
     Item it;
     bool have = next_item(it), more = false;
     int block = 0, page = 0, at = 0;
-    if (!have && lane == 0) ws.desc[part].n_parts = 0;
+    if (!have && lane == 0) ws.desc[part] = NO_JOIN;
     if (have) {
         open(it);
         more = blocks.next(c, it.kh, block, page, at);
@@ -477,6 +491,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache 
             }
             if (n_more) load_k(n_page, n_kh);
             if (more) {
+                const bool bad = not_finite(ka, va);
+                if (bad) ka = va = 0.f;
                 const float down = vs.take(va);
                 if (down != 1.0f) {
 #pragma unroll
@@ -484,6 +500,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache 
                 }
                 v8h pf[2];
                 softmax<NV>(s, qs * (ka * (1.0f / 127.0f)), vs, block * PAGE + PAGE - 1 > all_limit, my_limit - block * PAGE, m, l, o, pf);
+                if (bad && my_limit + 4 * (lane >> 4) >= block * PAGE) l = nan_f();
 #pragma unroll
                 for (int n = 0; n < NV; ++n) {
                     o[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8(vraw[n].x, vraw[n].y), pf[0], o[n], 0, 0, 0);
@@ -517,18 +534,39 @@ __device__ __forceinline__ u64 sum_vis(const RowInfo& x, const Cut& t, bool caus
     return s;
 }
 
-// Bound by the vector ALU (softmax, conversion), the matrix pipe and LDS reads about equally.  A block's codes are converted once
-// per workgroup into LDS (two buffers, one barrier per block), raw bytes two blocks ahead in registers; a wave's 32 query rows
-// share what it reads.
+// A wave's 32 query rows as operands of the 32x32x16 MFMA: operand s holds channels 16 s + 8 (lane / 32) + 0..7 of row lane % 32.
+template <int D, int DT>
+__device__ __forceinline__ float convert_q32(const uint4 (&raw)[D / 16], v8h (&qf)[D / 16]) {
+    if constexpr (DT == SPARGE_F16) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) __builtin_memcpy(&qf[s], &raw[s], 16);
+        return 1.0f;
+    } else {
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) top = max(top, top16(raw[s]));
+        top = max(top, __float_as_uint(other<32>(__uint_as_float(top))));
+        const int ex = exponent16(top);
+        const float down = __builtin_ldexpf(1.0f, -ex);
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) qf[s] = scaled8<DT>(raw[s], down);
+        return __builtin_ldexpf(1.0f, ex);
+    }
+}
+
+// Four waves share the blocks: their codes are converted once per workgroup into LDS, in the operand order of the 32x32x16 MFMA
+// (two buffers, one barrier a block; the raw bytes of the block after the next are on their way meanwhile), and every wave
+// reads them for its own 32 query rows.  In that MFMA's accumulators a lane owns one query (lane % 32) and, of every 16 keys,
+// 4 (lane / 32) + 0..3 and those + 8; V's operands are laid out for that order.
 template <int D, int DT>
 __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c, CacheAttn a, Rows which, const uint16_t* __restrict__ Q,
                                                                  uint16_t* __restrict__ O, Joint ws) {
-    constexpr int QT = WIDE_QT, NV = D / 16, KS = D / 32, RAW = D / 64;   // RAW: 16-byte pieces of K (of V) per thread
+    constexpr int KS = D / 16, NC = D / 32, RAW = D / 64;   // steps of K Q^T, channel tiles, 16-byte pieces of K (of V) per thread
     __shared__ u64 sums[4];
     __shared__ u64 found_rem;
     __shared__ int found_row;
-    __shared__ __align__(16) v8h lds_k[2][4 * KS * 64], lds_v[2][NV * 2 * 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    __shared__ __align__(16) v8h lds_k[2][2 * KS * 64], lds_v[2][NC * 4 * 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
     const Cut cut = cut_of(a.H / c.H_kv, WIDE_ROWS);
     const int heads = c.H_kv * cut.parts;
 
@@ -543,7 +581,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c,
     const int parts = wanted >= WIDE_WGS ? WIDE_WGS : wanted >= 8 ? static_cast<int>(wanted) & ~7 : wanted >= 1 ? static_cast<int>(wanted) : total > 0;
     const int bid = blockIdx.x;
     if (bid >= parts) {
-        if (tid == 0) ws.desc[bid].n_parts = 0;
+        if (tid == 0) ws.desc[bid] = NO_JOIN;
         return;
     }
     const int part = parts >= 8 ? (bid & 7) * (parts / 8) + (bid >> 3) : bid;
@@ -562,7 +600,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c,
     __syncthreads();
     int r = uniform(found_row);
     u64 rem = uniform(found_rem), pos = lo;
-    JoinDesc join = {0, 0, 0, 0, 0};
+    JoinDesc join = NO_JOIN;
 
     while (pos < hi && r < c.R) {
         const RowInfo x = uniform(row_info(c, a, cut, which, r));
@@ -580,34 +618,30 @@ __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c,
             if (sum_vis(x, cut, a.causal, mid) <= in) i = mid; else up = mid;
         }
         const int x0 = static_cast<int>(in - sum_vis(x, cut, a.causal, i));
-        const int ntok = min(cut.TT, x.n - i * cut.TT);
+        const int ntok = min(cut.TT, x.n - i * cut.TT), token0 = x.first + i * cut.TT;
+        const int kh = head / cut.parts, g0 = (head - kh * cut.parts) * WIDE_ROWS, n_heads = min(cut.Gp, cut.G - g0);
         const int vis = a.causal ? x.p0 + i * cut.TT + ntok : x.len;
         const int take = static_cast<int>(min(static_cast<u64>(vis - x0), hi - pos)), x1 = x0 + take;
         const int b0 = x0 / PAGE, b1 = x1 == vis ? (vis + PAGE - 1) / PAGE : x1 / PAGE;
         const bool whole = x0 == 0 && x1 == vis;
-        if (pos == lo && x0 > 0) join = boundary(total, parts, part, lo - x0, lo - x0 + vis, r, head, i);
+        if (pos == lo && x0 > 0) join = boundary(total, parts, part, lo - x0, lo - x0 + vis, token0, ntok, kh * cut.G + g0, n_heads);
 
-        const int kh = head / cut.parts, gpart = head - kh * cut.parts;
-        const int n_rows = ntok * cut.Gp, row0 = wave * 16 * QT + (lane & 15);
-        int limit[QT];
-        bool valid[QT];
-        uint4 q_raw[QT][KS];
-        // the wave's rows: the least and the largest key that one of them sees last
-        const int w0 = wave * 16 * QT, w1 = min(w0 + 16 * QT, n_rows) - 1;
-        const int tok_lo = w0 / cut.Gp, tok_hi = max(w1, 0) / cut.Gp;
-        const int lim_lo = a.causal ? min(x.p0 + i * cut.TT + tok_lo, x.len - 1) : x.len - 1;
-        const int lim_hi = w1 < w0 ? -1 : a.causal ? min(x.p0 + i * cut.TT + tok_hi, x.len - 1) : x.len - 1;
+        // this wave's rows, the lane's one of them, and the least and the largest key that a row sees last
+        const int n_rows = ntok * cut.Gp, w0 = wave * 32, w1 = min(w0 + 32, n_rows) - 1;
+        const int row = w0 + (lane & 31), tok = row / cut.Gp, g = row - tok * cut.Gp;
+        const bool valid = row < n_rows && g < n_heads;
+        const int first_limit = a.causal ? x.p0 + i * cut.TT : x.len - 1;
+        const int limit = !valid ? -1 : min(first_limit + (a.causal ? tok : 0), x.len - 1);
+        const int lim_lo = min(first_limit + (a.causal ? w0 / cut.Gp : 0), x.len - 1);
+        const int lim_hi = w1 < w0 ? -1 : min(first_limit + (a.causal ? w1 / cut.Gp : 0), x.len - 1);
         Blocks blocks;
         blocks.open(c, a, r, kh, b0, min(b1, (x.len + PAGE - 1) / PAGE));
-        long long out_at[QT];
+        const long long token = token0 + tok, hd = kh * cut.G + g0 + g;
+        uint4 q_raw[KS];
 #pragma unroll
-        for (int q = 0; q < QT; ++q) {
-            const int row = row0 + 16 * q, tok = row / cut.Gp, g = gpart * WIDE_ROWS + row - tok * cut.Gp;
-            valid[q] = row < n_rows && g < cut.G;
-            limit[q] = (!valid[q] ? -1 : a.causal ? min(x.p0 + i * cut.TT + tok, x.len - 1) : x.len - 1) - 4 * (lane >> 4);
-            const long long token = x.first + i * cut.TT + tok, hd = kh * cut.G + g;
-            out_at[q] = token * a.o_sn + hd * a.o_sh;
-            load_q<D>(q_raw[q], Q + token * a.q_sn + hd * a.q_sh + 16 * (lane >> 4), valid[q]);
+        for (int s = 0; s < KS; ++s) {
+            q_raw[s] = make_uint4(0u, 0u, 0u, 0u);
+            if (valid) q_raw[s] = *reinterpret_cast<const uint4*>(Q + token * a.q_sn + hd * a.q_sh + 16 * s + 8 * half);
         }
 
         uint4 kraw[RAW], vraw[RAW];
@@ -619,14 +653,26 @@ __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c,
                 vraw[n] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(c.v) + at + n * 4096);
             }
         };
-        auto convert = [&](int buf) {   // piece p = tid + 256 n of 64 lanes each: operands 2 (p / 64) and 2 (p / 64) + 1
+        auto convert = [&](int buf) {
+            const int l16 = lane & 15, gr = lane >> 4;
 #pragma unroll
             for (int n = 0; n < RAW; ++n) {
-                const int op = 2 * (wave + 4 * n);
-                lds_k[buf][op * 64 + lane] = codes8(kraw[n].x, kraw[n].y);
-                lds_k[buf][(op + 1) * 64 + lane] = codes8(kraw[n].z, kraw[n].w);
-                lds_v[buf][op * 64 + lane] = codes8(vraw[n].x, vraw[n].y);
-                lds_v[buf][(op + 1) * 64 + lane] = codes8(vraw[n].z, vraw[n].w);
+                const int piece = wave + 4 * n;
+                // K: keys 16 t + l16, channels 64 e + 16 gr + 0..15: step 4 e + gr of key tile t / 2, eight channels a half
+                const int t = piece / (D / 64), e = piece - t * (D / 64);
+                v8h* k = &lds_k[buf][((t >> 1) * KS + 4 * e + gr) * 64 + 16 * (t & 1) + l16];
+                k[0] = codes8(kraw[n].x, kraw[n].y);
+                k[32] = codes8(kraw[n].z, kraw[n].w);
+                // V: channel 16 piece + l16, keys 16 t + 4 gr + 0..3 in word t: step t, half gr % 2, place 4 (gr / 2)
+                uint2* v = reinterpret_cast<uint2*>(&lds_v[buf][(piece >> 1) * 4 * 64 + 16 * (piece & 1) + l16 + 32 * (gr & 1)]) + (gr >> 1);
+                const v8h v01 = codes8(vraw[n].x, vraw[n].y), v23 = codes8(vraw[n].z, vraw[n].w);
+                uint4 w01, w23;
+                __builtin_memcpy(&w01, &v01, 16);
+                __builtin_memcpy(&w23, &v23, 16);
+                v[0] = make_uint2(w01.x, w01.y);
+                v[128] = make_uint2(w01.z, w01.w);
+                v[256] = make_uint2(w23.x, w23.y);
+                v[384] = make_uint2(w23.z, w23.w);
             }
         };
         int block = 0, page = 0, at = 0, n_block = 0, n_at = 0;
@@ -636,16 +682,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c,
             load_raw(page);
             ka = blocks.ka(at), va = blocks.va(at);
         }
-        v8h qf[QT][KS];
-        float qs[QT], m[QT], l[QT];
-        v4f o[QT][NV];
+        v8h qf[KS];
+        const float qs = a.scale_log2 * (1.0f / 127.0f) * convert_q32<D, DT>(q_raw, qf);
+        float m = FAR, l = 0.f;
+        v16f o[NC];
 #pragma unroll
-        for (int q = 0; q < QT; ++q) {
-            qs[q] = a.scale_log2 * convert_q<D, DT>(q_raw[q], qf[q]);
-            m[q] = FAR, l[q] = 0.f;
+        for (int n = 0; n < NC; ++n)
 #pragma unroll
-            for (int n = 0; n < NV; ++n) o[q][n] = {0.f, 0.f, 0.f, 0.f};
-        }
+            for (int e = 0; e < 16; ++e) o[n][e] = 0.f;
         VScale vs;
         if (more) {
             convert(0);
@@ -656,6 +700,59 @@ __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c,
             }
         }
         __syncthreads();
+        auto step = [&](bool masked, int buf) {
+            v16f s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+#pragma unroll
+                for (int e = 0; e < KS; ++e) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_k[buf][(t * KS + e) * 64 + lane], qf[e], s[t], 0, 0, 0);
+            }
+            float cq = qs * ka;
+            if (cq == 0.f) cq = 1e-37f;   // a block of zeros: -inf stays what it is and becomes a weight of 0
+            const int last = limit - block * PAGE - 4 * half;   // key 32 t + 8 (e / 4) + e % 4 of the lane's
+            if (masked) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (32 * t + 8 * (e >> 2) + (e & 3) > last) s[t][e] = -INFINITY;
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
+            top = fmaxf(top, other<32>(top)) * cq;
+            float down = vs.take(va);
+            const float to = fmaxf(m, top);
+            if (__any(top > m + SLACK) || down != 1.0f) {
+                const bool moves = __any(top > m + SLACK);
+                const float dm = moves ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
+                if (moves) m = to;
+                l *= dm;
+                down *= dm;
+#pragma unroll
+                for (int n = 0; n < NC; ++n) o[n] *= down;
+            }
+            const float from = vs.f_log2 - m;
+            float sum = 0.f;
+            v8h pf[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                float w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + e], cq, from));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += w[e];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pf[u][e] = static_cast<_Float16>(w[e]);
+#pragma unroll
+                for (int n = 0; n < NC; ++n) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_v[buf][(n * 4 + u) * 64 + lane], pf[u], o[n], 0, 0, 0);
+            }
+            l += sum * vs.f_inv;
+        };
         for (int buf = 0; more; buf ^= 1) {
             // the next block's bytes into the other buffer, the one after it on its way
             int nn_block = 0, nn_at = 0;
@@ -670,52 +767,41 @@ __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c,
                 }
             }
             if (block * PAGE <= lim_hi) {
-                v4f s[QT][4];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-#pragma unroll
-                    for (int q = 0; q < QT; ++q) s[q][t] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int e = 0; e < KS; ++e) {
-                        const v8h k = lds_k[buf][(t * KS + e) * 64 + lane];
-#pragma unroll
-                        for (int q = 0; q < QT; ++q) s[q][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[q][e], s[q][t], 0, 0, 0);
-                    }
-                }
-                const float down = vs.take(va);
-                if (down != 1.0f) {
-#pragma unroll
-                    for (int q = 0; q < QT; ++q)
-#pragma unroll
-                        for (int n = 0; n < NV; ++n) o[q][n] *= down;
-                }
-                const bool masked = block * PAGE + PAGE - 1 > lim_lo;
-                const float sk = ka * (1.0f / 127.0f);
-                v8h pf[QT][2];
-#pragma unroll
-                for (int q = 0; q < QT; ++q) softmax<NV>(s[q], qs[q] * sk, vs, masked, limit[q] - block * PAGE, m[q], l[q], o[q], pf[q]);
-#pragma unroll
-                for (int n = 0; n < NV; ++n) {
-                    const v8h v0 = lds_v[buf][2 * n * 64 + lane], v1 = lds_v[buf][(2 * n + 1) * 64 + lane];
-#pragma unroll
-                    for (int q = 0; q < QT; ++q) {
-                        o[q][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[q][0], o[q][n], 0, 0, 0);
-                        o[q][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[q][1], o[q][n], 0, 0, 0);
-                    }
-                }
+                const bool bad = not_finite(ka, va);
+                if (bad) ka = va = 0.f;
+                step(block * PAGE + PAGE - 1 > lim_lo, buf);
+                if (bad && limit >= block * PAGE) l = nan_f();
             }
             __syncthreads();
             more = n_more, block = n_block, ka = n_ka, va = n_va;
             n_more = nn_more, n_block = nn_block, n_ka = nn_ka, n_va = nn_va;
         }
 
-        const float o_scale = vs.ref * (1.0f / (127.0f * 256.0f));
+        l += other<32>(l);
+        if (valid) {
+            const float o_scale = vs.ref * (1.0f / (127.0f * 256.0f));
+            const float inv = o_scale / l;
+            uint16_t* out = O + token * a.o_sn + hd * a.o_sh + 4 * half;
+            const long long row_at = static_cast<long long>(2 * part + (x0 > 0 ? 0 : 1)) * WIDE_ROWS + row;
 #pragma unroll
-        for (int q = 0; q < QT; ++q) {
-            l[q] = sum_groups(l[q]);
-            if (!valid[q]) continue;
-            if (whole) store_whole<NV, DT>(o[q], l[q], o_scale, O + out_at[q] + 4 * (lane >> 4));
-            else store_part<NV>(o[q], m[q], l[q], o_scale, ws, static_cast<long long>(2 * part + (x0 > 0 ? 0 : 1)) * WIDE_ROWS + row0 + 16 * q);
+            for (int n = 0; n < NC; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {   // channels 32 n + 8 e + 4 half + 0..3
+                    v4f y;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) y[k] = o[n][4 * e + k];
+                    if (whole) {
+                        uint16_t h[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) h[k] = l == 0.f ? 0 : cvt_to16<DT>(y[k] * inv);
+                        uint2 w;
+                        __builtin_memcpy(&w, h, 8);
+                        *reinterpret_cast<uint2*>(out + 32 * n + 8 * e) = w;
+                    } else {
+                        *reinterpret_cast<v4f*>(ws.o + row_at * D + 32 * n + 8 * e + 4 * half) = y * o_scale;
+                    }
+                }
+            if (!whole && half == 0) ws.ml[2 * row_at] = m, ws.ml[2 * row_at + 1] = l;
         }
         pos += take;
         rem += take;
@@ -725,71 +811,73 @@ __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c,
 
 // ---- join ----------------------------------------------------------------------------------------------------------
 
-// Joins an item that several parts hold, in their order: workgroup x looks at `descs` parts that might be the first one to
-// begin inside an item, and takes every JOIN_Y-th row.  A row's channels take D / 4 threads, its parts are dealt out over
-// the 1024 / D groups of that many, whose results go through LDS; where there are few parts the groups take rows instead.
-template <int D, int DT, int ROWS>
-__global__ __launch_bounds__(256) void cache_join_kernel(sparge_cache c, CacheAttn a, Rows which, int descs, uint16_t* __restrict__ O, Joint ws) {
-    constexpr int TPR = D / 4, GROUPS = 256 / TPR;   // threads per row, groups of them
-    __shared__ __align__(16) v4f lds_o[GROUPS][TPR];
-    __shared__ float lds_m[GROUPS], lds_l[GROUPS];
-    const int grp = threadIdx.x / TPR, ch = (threadIdx.x % TPR) * 4;
-    const Cut cut = cut_of(a.H / c.H_kv, ROWS);
-    for (int n = 0; n < descs; ++n) {
-        const JoinDesc d = ws.desc[blockIdx.x * descs + n];
-        if (d.n_parts == 0) continue;
-        const RowInfo x = row_info(c, a, cut, which, d.row);
-        const int kh = d.head / cut.parts, gpart = d.head - kh * cut.parts;
-        const int n_rows = min(cut.TT, x.n - d.tile * cut.TT) * cut.Gp;
-        // the item's start is the second result of the part before the first boundary, the rest are first results
-        auto slot = [&](int k) { return static_cast<long long>(k == 0 ? 2 * (d.part - 1) + 1 : 2 * (d.part + k - 1)) * ROWS; };
-        const bool deal = d.n_parts > 4;
-        const int k0 = deal ? grp : 0, ks = deal ? GROUPS : 1;
-        for (int base = 0; base < n_rows; base += deal ? JOIN_Y : JOIN_Y * GROUPS) {
-            const int row = base + (deal ? static_cast<int>(blockIdx.y) : static_cast<int>(blockIdx.y) * GROUPS + grp);
-            const int tok = row / cut.Gp, g = gpart * ROWS + row - tok * cut.Gp;
-            const bool there = row < n_rows && g < cut.G;
-            float m = FAR, l = 0.f;
-            v4f o = {0.f, 0.f, 0.f, 0.f};
-            if (there) {
-                float top = FAR;
-#pragma unroll 4
-                for (int k = k0; k < d.n_parts; k += ks) top = fmaxf(top, ws.ml[2 * (slot(k) + row)]);
-                m = top;
-#pragma unroll 4
-                for (int k = k0; k < d.n_parts; k += ks) {
-                    const long long at = slot(k) + row;
-                    const float w = __builtin_amdgcn_exp2f(ws.ml[2 * at] - m);
-                    l += ws.ml[2 * at + 1] * w;
-                    o += *reinterpret_cast<const v4f*>(ws.o + at * D + ch) * w;
-                }
-            }
-            if (deal) {
-                __syncthreads();
-                lds_o[grp][ch / 4] = o;
-                if (ch == 0) lds_m[grp] = m, lds_l[grp] = l;
-                __syncthreads();
-                if (grp == 0) {
-                    for (int k = 1; k < GROUPS; ++k) m = fmaxf(m, lds_m[k]);
-                    l = 0.f, o = {0.f, 0.f, 0.f, 0.f};
-                    for (int k = 0; k < GROUPS; ++k) {
-                        const float w = __builtin_amdgcn_exp2f(lds_m[k] - m);
-                        l += lds_l[k] * w;
-                        o += lds_o[k][ch / 4] * w;
-                    }
-                }
-            }
-            if (there && (!deal || grp == 0)) {
-                uint16_t h[4];
+// Joins items that several parts hold, each in its parts' order.  An item's rows are cut into chunks of channels, which the waves
+// of the parts that begin inside the item deal out among them.  A wave's lanes take 4 channels each of 256 / PG, and the
+// PG groups of lanes every PG-th part, up to eight of them in one round trip to memory.
+template <int D, int DT, int ROWS, int PG>
+__device__ __forceinline__ void join_item(const JoinDesc& d, int me, int workers, int Gp, const CacheAttn& a, uint16_t* O, const Joint& ws) {
+    constexpr int LANES = 64 / PG;
+    const int lane = threadIdx.x & 63, grp = lane / LANES, n_chunks = (d.n_tok * Gp * D * PG + 255) / 256;
+    for (int chunk = me; chunk < n_chunks; chunk += workers) {
+        const int flat = chunk * (256 / PG) + (lane % LANES) * 4, row = flat / D, ch = flat % D;
+        const int tok = row / Gp, g = row - tok * Gp;
+        const bool there = tok < d.n_tok && g < d.n_heads;
+        float m = FAR, l = 0.f;
+        v4f o = {0.f, 0.f, 0.f, 0.f};
+        for (int k0 = grp; k0 < d.n_parts; k0 += 8 * PG) {
+            float pm[8], pl[8];
+            v4f po[8];
+            float top = m;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) h[e] = l == 0.f ? 0 : cvt_to16<DT>(o[e] / l);
-                uint2 w;
-                __builtin_memcpy(&w, h, 8);
-                *reinterpret_cast<uint2*>(O + static_cast<long long>(x.first + d.tile * cut.TT + tok) * a.o_sn +
-                                          static_cast<long long>(kh * cut.G + g) * a.o_sh + ch) = w;
+            for (int e = 0; e < 8; ++e) {
+                const int k = k0 + e * PG;
+                pm[e] = FAR, pl[e] = 0.f, po[e] = {0.f, 0.f, 0.f, 0.f};
+                if (there && k < d.n_parts) {
+                    // the item's start is the second result of the part before the first boundary, the rest are first results
+                    const long long at = static_cast<long long>(k == 0 ? 2 * (d.first - 1) + 1 : 2 * (d.first + k - 1)) * ROWS + row;
+                    pm[e] = ws.ml[2 * at], pl[e] = ws.ml[2 * at + 1];
+                    po[e] = *reinterpret_cast<const v4f*>(ws.o + at * D + ch);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, pm[e]);
+            const float down = __builtin_amdgcn_exp2f(m - top);
+            l *= down, o *= down, m = top;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float w = __builtin_amdgcn_exp2f(pm[e] - top);
+                l += pl[e] * w;
+                o += po[e] * w;
             }
         }
+#pragma unroll
+        for (int x = LANES; x < 64; x <<= 1) {
+            const float om = __shfl_xor(m, x), ol = __shfl_xor(l, x), top = fmaxf(m, om);
+            const float wa = __builtin_amdgcn_exp2f(m - top), wb = __builtin_amdgcn_exp2f(om - top);
+            l = l * wa + ol * wb;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = o[e] * wa + __shfl_xor(o[e], x) * wb;
+            m = top;
+        }
+        if (there && grp == 0) {
+            uint16_t h[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = l == 0.f ? 0 : cvt_to16<DT>(o[e] / l);
+            uint2 w;
+            __builtin_memcpy(&w, h, 8);
+            *reinterpret_cast<uint2*>(O + static_cast<long long>(d.token + tok) * a.o_sn + static_cast<long long>(d.head + g) * a.o_sh + ch) = w;
+        }
     }
+}
+// WAVES: of a workgroup, for one description
+template <int D, int DT, int ROWS, int WAVES>
+__global__ __launch_bounds__(256) void cache_join_kernel(sparge_cache c, CacheAttn a, uint16_t* __restrict__ O, Joint ws) {
+    const int wave = uniform(static_cast<int>(threadIdx.x) >> 6);
+    const JoinDesc d = ws.desc[(blockIdx.x * 4 + wave) / WAVES];
+    if (d.n_parts == 0) return;
+    const int Gp = cut_of(a.H / c.H_kv, ROWS).Gp, me = (d.part - d.first) * WAVES + wave % WAVES, workers = (d.n_parts - 1) * WAVES;
+    if (d.n_parts <= 4) join_item<D, DT, ROWS, 1>(d, me, workers, Gp, a, O, ws);
+    else join_item<D, DT, ROWS, 8>(d, me, workers, Gp, a, O, ws);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -815,12 +903,12 @@ void launch(const sparge_cache& c, const CacheAttn& a, bool narrow, bool wide, c
     if (narrow) {
         const Rows which = wide ? FEW_ROWS : ALL_ROWS;
         hipLaunchKernelGGL((cache_attn_narrow_kernel<D, DT>), dim3(NARROW_WGS), dim3(256), 0, st, c, a, which, Q, O, j);
-        hipLaunchKernelGGL((cache_join_kernel<D, DT, NARROW_ROWS>), dim3(NARROW_WGS, JOIN_Y), dim3(256), 0, st, c, a, which, 4, O, j);
+        hipLaunchKernelGGL((cache_join_kernel<D, DT, NARROW_ROWS, 1>), dim3(NARROW_PARTS / 4), dim3(256), 0, st, c, a, O, j);
     }
     if (wide) {
         const Rows which = narrow ? MANY_ROWS : ALL_ROWS;
         hipLaunchKernelGGL((cache_attn_wide_kernel<D, DT>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, which, Q, O, j);
-        hipLaunchKernelGGL((cache_join_kernel<D, DT, WIDE_ROWS>), dim3(WIDE_WGS, JOIN_Y), dim3(256), 0, st, c, a, which, 1, O, j);
+        hipLaunchKernelGGL((cache_join_kernel<D, DT, WIDE_ROWS, 4>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, O, j);
     }
 }
 
