@@ -429,7 +429,8 @@ class SpargeCache:
     """The tensors of one layer's paged 8-bit K/V cache (sparge.h, sparge_cache).  `book` holds what changes from step to step but
     the pages (n_free, length [R], free_pages [n_pages], table [R, max_blocks], int32, one tensor): a copy of it is a point to
     go back to.  share: a cache of the same rows and pages whose book this one uses, too (the layers of a model plan once
-    per step).  k_shift: fp32 [R, H_kv, d] or None; it must not change while rows hold tokens."""
+    per step).  k_shift: fp32 [R, H_kv, d] or None; it must not change while rows hold tokens.  The tensors stay the ones
+    made here: change what they hold, do not replace them."""
 
     def __init__(self, rows: int, kv_heads: int, head_dim: int, n_pages: int, max_blocks: int, dtype: torch.dtype = torch.bfloat16,
                  device="cuda", k_shift: Optional[torch.Tensor] = None, share: Optional["SpargeCache"] = None):
@@ -468,32 +469,78 @@ class SpargeCache:
                               *[None if t is None else t.data_ptr() for t in (
                                   self.k, self.v, self.k_amax, self.v_amax, self.k_tail, self.v_tail, self.table, self.length,
                                   self.free_pages, self.n_free, k_shift)])
+        self._ref = ctypes.byref(self._struct)
+        self._ws_bytes = {}     # query heads -> sparge_cache_attn_workspace_bytes
 
 
 class CachePlan:
-    """What sparge_cache_plan gives: cu int32 [R + 1], slots and req int32 [n_slots], status int32 [2]."""
+    """What sparge_cache_plan gives, int32 on the GPU: cu [R + 1], slots and req [n_slots], status [2]."""
 
     def __init__(self, cu: torch.Tensor, slots: torch.Tensor, req: torch.Tensor, status: torch.Tensor):
-        self.cu, self.slots, self.req, self.status = cu, slots, req, status
+        n = slots.numel()
+        for name, t, shape in (("cu", cu, (cu.numel(),)), ("slots", slots, (n,)), ("req", req, (n,)), ("status", status, (2,))):
+            _array(t, torch.int32, shape, cu.device, f"plan.{name}")
+        self._parts = (cu, slots, req, status)
+        self._set(cu.device, cu.numel() - 1, n, *[t.data_ptr() for t in self._parts])
+
+    def _set(self, device, rows, n_slots, cu, slots, req, status):
+        self.device, self.rows, self.n_slots = device, rows, n_slots
+        self._cu, self._slots, self._req, self._status = cu, slots, req, status   # addresses
+
+    @classmethod
+    def _new(cls, cache: SpargeCache, n_slots: int) -> "CachePlan":
+        """One tensor for all four (an allocation costs a small step as much as its kernel); they are cut out when asked for."""
+        self = cls.__new__(cls)
+        R = cache.rows
+        self._parts, self._buffer = None, torch.empty(R + 3 + 2 * n_slots, dtype=torch.int32, device=cache.device)
+        at = self._buffer.data_ptr()
+        self._set(cache.device, R, n_slots, at, at + 4 * (R + 3), at + 4 * (R + 3 + n_slots), at + 4 * (R + 1))
+        return self
+
+    def _part(self, i: int) -> torch.Tensor:
+        if self._parts is None:
+            cu, status, slots, req = self._buffer.split([self.rows + 1, 2, self.n_slots, self.n_slots])
+            self._parts = (cu, slots, req, status)
+        return self._parts[i]
+
+    cu = property(lambda self: self._part(0))
+    slots = property(lambda self: self._part(1))
+    req = property(lambda self: self._part(2))
+    status = property(lambda self: self._part(3))
 
 
 def _array(t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], device: torch.device, name: str) -> None:
-    if tuple(t.shape) != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
         raise SpargeError(f"{name} must be a contiguous {dtype} {list(shape)} tensor on {device}")
 
 
-def _tokens(t: torch.Tensor, cache: SpargeCache, n_slots: int, heads: Optional[int], name: str) -> None:
-    if t.dim() != 3 or t.shape[0] != n_slots or t.shape[2] != cache.head_dim or (heads is not None and t.shape[1] != heads):
-        raise SpargeError(f"{name} must be [{n_slots}, {'H' if heads is None else heads}, {cache.head_dim}], not {list(t.shape)}")
-    if t.dtype != cache.dtype or t.device != cache.device:
+def _tokens(t: torch.Tensor, cache: SpargeCache, n_slots: int, heads: int, name: str) -> Tuple[int, int, int]:
+    """-> address, strides per token and head"""
+    if t.shape != (n_slots, heads, cache.head_dim):
+        raise SpargeError(f"{name} must be [{n_slots}, {heads}, {cache.head_dim}], not {list(t.shape)}")
+    if t.dtype is not cache.dtype or t.device != cache.device:
         raise SpargeError(f"{name} must be {cache.dtype} on {cache.device}")
-    if t.stride(2) != 1 and t.numel():
+    sn, sh, sd = t.stride()
+    if sd != 1 and n_slots:
         raise SpargeError("the head dimension must be contiguous")
+    return t.data_ptr(), sn, sh
 
 
-def _on(cache: SpargeCache):
-    """The cache's device made current for a call (and the stream that is current there)."""
-    return torch.cuda.device(cache.device)
+def _call(cache: SpargeCache, f, *args) -> None:
+    """One entry point on the cache's device and the stream that is current there.  (Making the device current and asking for
+    its stream object cost 6 us, as much as a small step's kernels; both are left out where they change nothing.)"""
+    index = cache.device.index
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return _call(cache, f, *args)
+    rc = f(cache._ref, *args, torch._C._cuda_getCurrentRawStream(index))
+    if rc != 0:
+        _check(rc)
+
+
+def _same_rows(cache: SpargeCache, plan: CachePlan) -> None:
+    if plan.rows != cache.rows or plan.device != cache.device:
+        raise SpargeError(f"the plan is for {plan.rows} rows on {plan.device}, the cache has {cache.rows} on {cache.device}")
 
 
 def sparge_cache_plan(cache: SpargeCache, new_len: torch.Tensor, n_slots: int, release: Optional[torch.Tensor] = None,
@@ -504,33 +551,26 @@ def sparge_cache_plan(cache: SpargeCache, new_len: torch.Tensor, n_slots: int, r
     _array(new_len, torch.int32, (cache.rows,), cache.device, "new_len")
     if release is not None:
         _array(release, torch.uint8, (cache.rows,), cache.device, "release")
+    if n_slots < 0:
+        raise SpargeError(f"n_slots = {n_slots} is negative")
     if out is None:
-        new = lambda n: torch.empty(n, dtype=torch.int32, device=cache.device)
-        out = CachePlan(new(cache.rows + 1), new(n_slots), new(n_slots), new(2))
-    for name, t, n in (("cu", out.cu, cache.rows + 1), ("slots", out.slots, n_slots), ("req", out.req, n_slots), ("status", out.status, 2)):
-        _array(t, torch.int32, (n,), cache.device, f"plan.{name}")
-    with _on(cache):
-        _check(load_library().sparge_cache_plan(ctypes.byref(cache._struct), _ptr(new_len), _ptr(release), n_slots, _ptr(out.cu),
-                                                _ptr(out.slots), _ptr(out.req), _ptr(out.status), _stream()))
+        out = CachePlan._new(cache, n_slots)
+    else:
+        _same_rows(cache, out)
+        if out.n_slots != n_slots:
+            raise SpargeError(f"the plan given has {out.n_slots} slots, not {n_slots}")
+    _call(cache, load_library().sparge_cache_plan, new_len.data_ptr(), None if release is None else release.data_ptr(), n_slots,
+          out._cu, out._slots, out._req, out._status)
     return out
 
 
 def sparge_cache_append(cache: SpargeCache, K: torch.Tensor, V: torch.Tensor, plan: CachePlan) -> None:
     """Stores the step's tokens, K, V [n_slots, H_kv, d], where the plan says."""
-    n = plan.slots.numel()
-    _tokens(K, cache, n, cache.kv_heads, "K")
-    _tokens(V, cache, n, cache.kv_heads, "V")
-    _plan_arrays(cache, plan)
-    with _on(cache):
-        _check(load_library().sparge_cache_append(ctypes.byref(cache._struct), _ptr(K), _ptr(V), n, K.stride(0), K.stride(1),
-                                                  V.stride(0), V.stride(1), _ptr(plan.cu), _ptr(plan.slots), _ptr(plan.req), _stream()))
-
-
-def _plan_arrays(cache: SpargeCache, plan: CachePlan) -> None:
-    n = plan.slots.numel()
-    _array(plan.cu, torch.int32, (cache.rows + 1,), cache.device, "plan.cu")
-    _array(plan.slots, torch.int32, (n,), cache.device, "plan.slots")
-    _array(plan.req, torch.int32, (n,), cache.device, "plan.req")
+    _same_rows(cache, plan)
+    n = plan.n_slots
+    k, k_sn, k_sh = _tokens(K, cache, n, cache.kv_heads, "K")
+    v, v_sn, v_sh = _tokens(V, cache, n, cache.kv_heads, "V")
+    _call(cache, load_library().sparge_cache_append, k, v, n, k_sn, k_sh, v_sn, v_sh, plan._cu, plan._slots, plan._req)
 
 
 def sparge_cache_read(cache: SpargeCache, slots: torch.Tensor, req: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
@@ -538,27 +578,30 @@ def sparge_cache_read(cache: SpargeCache, slots: torch.Tensor, req: Optional[tor
     """-> K, V [n, H_kv, d]: the values that the codes of these slots (int32 [n]) stand for, in fp32 or the cache's dtype (default).
     req: the slots' rows, int32 [n], for a cache with k_shift.  Outputs of slots outside the pool are left as they were."""
     dtype = dtype or cache.dtype
-    if dtype not in (torch.float32, cache.dtype):
+    if dtype is not torch.float32 and dtype is not cache.dtype:
         raise SpargeError(f"dtype {dtype} is neither fp32 nor the cache's {cache.dtype}")
-    if slots.dim() != 1:
-        raise SpargeError("slots must be a vector")
     n = slots.numel()
     _array(slots, torch.int32, (n,), cache.device, "slots")
     if req is not None:
         _array(req, torch.int32, (n,), cache.device, "req")
-    K, V = out if out is not None else (torch.empty((n, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.device) for _ in range(2))
-    _array(K, dtype, (n, cache.kv_heads, cache.head_dim), cache.device, "K")
-    _array(V, dtype, (n, cache.kv_heads, cache.head_dim), cache.device, "V")
-    code = 2 if dtype == torch.float32 else cache._struct.dtype
-    with _on(cache):
-        _check(load_library().sparge_cache_read(ctypes.byref(cache._struct), _ptr(slots), _ptr(req), n, code, _ptr(K), _ptr(V), _stream()))
+    shape = (n, cache.kv_heads, cache.head_dim)
+    if out is None:
+        K, V = (torch.empty(shape, dtype=dtype, device=cache.device) for _ in range(2))
+    else:
+        K, V = out
+        _array(K, dtype, shape, cache.device, "K")
+        _array(V, dtype, shape, cache.device, "V")
+    _call(cache, load_library().sparge_cache_read, slots.data_ptr(), None if req is None else req.data_ptr(), n,
+          2 if dtype is torch.float32 else cache._struct.dtype, K.data_ptr(), V.data_ptr())
     return K, V
 
 
 def sparge_cache_attn_workspace_bytes(cache: SpargeCache, H: int) -> int:
-    n = ctypes.c_size_t(0)
-    _check(load_library().sparge_cache_attn_workspace_bytes(ctypes.byref(cache._struct), H, ctypes.byref(n)))
-    return int(n.value)
+    if H not in cache._ws_bytes:
+        n = ctypes.c_size_t(0)
+        _check(load_library().sparge_cache_attn_workspace_bytes(cache._ref, H, ctypes.byref(n)))
+        cache._ws_bytes[H] = int(n.value)
+    return cache._ws_bytes[H]
 
 
 def sparge_cache_attn(cache: SpargeCache, Q: torch.Tensor, plan: CachePlan, causal: bool = True, sm_scale: float = 0.0,
@@ -566,23 +609,23 @@ def sparge_cache_attn(cache: SpargeCache, Q: torch.Tensor, plan: CachePlan, caus
                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the step's tokens, Q [n_slots, H, d], over the cache (after sparge_cache_append).  mask: uint8
     [R, H_kv, max_blocks], 0 = no key of that block is seen.  -> O like Q (rows that are no token of the step: as they were)."""
-    n = plan.slots.numel()
-    _tokens(Q, cache, n, None, "Q")
-    _plan_arrays(cache, plan)
+    _same_rows(cache, plan)
+    n = plan.n_slots
+    if Q.dim() != 3:
+        raise SpargeError("Q must be [n_slots, H, d]")
     H = Q.shape[1]
+    q, q_sn, q_sh = _tokens(Q, cache, n, H, "Q")
     if mask is not None:
         _array(mask, torch.uint8, (cache.rows, cache.kv_heads, cache.max_blocks), cache.device, "mask")
     O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device) if out is None else out
-    _tokens(O, cache, n, H, "out")
+    o, o_sn, o_sh = _tokens(O, cache, n, H, "out")
     need = sparge_cache_attn_workspace_bytes(cache, H)
     if ws is None:
         ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
     elif ws.device != cache.device or not ws.is_contiguous():
         raise SpargeError(f"ws must be contiguous on {cache.device}")
-    with _on(cache):
-        _check(load_library().sparge_cache_attn(ctypes.byref(cache._struct), _ptr(Q), n, H, Q.stride(0), Q.stride(1), _ptr(plan.cu),
-                                                _ptr(mask), float(sm_scale), int(causal), _ptr(O), O.stride(0), O.stride(1),
-                                                _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    _call(cache, load_library().sparge_cache_attn, q, n, H, q_sn, q_sh, plan._cu, None if mask is None else mask.data_ptr(), sm_scale,
+          int(causal), o, o_sn, o_sh, ws.data_ptr(), ws.numel() * ws.element_size())
     return O
 
 

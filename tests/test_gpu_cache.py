@@ -388,8 +388,11 @@ def test_the_binding_refuses(sp):
     c, new = m.cache, m.i32([1, 1])
     x = torch.zeros(5, 2, 64, dtype=torch.bfloat16, device="cuda")
     q = torch.zeros(5, 4, 64, dtype=torch.bfloat16, device="cuda")
-    cpu = sp.CachePlan(plan.cu.cpu(), plan.slots, plan.req, plan.status)
-    calls = [lambda: sp.sparge_cache_plan(c, new.long(), 5), lambda: sp.sparge_cache_plan(c, new[:1], 5), lambda: sp.sparge_cache_plan(c, new.cpu(), 5),
+    cpu = sp.CachePlan(plan.cu.cpu(), plan.slots.cpu(), plan.req.cpu(), plan.status.cpu())
+    other = sp.CachePlan(torch.cat([plan.cu, plan.cu[-1:]]), plan.slots, plan.req, plan.status)     # of three rows
+    calls = [lambda: sp.CachePlan(plan.cu.cpu(), plan.slots, plan.req, plan.status), lambda: sp.CachePlan(plan.cu, plan.slots, plan.req[1:], plan.status),
+             lambda: sp.CachePlan(plan.cu.long(), plan.slots, plan.req, plan.status), lambda: sp.sparge_cache_append(c, x, x, other),
+             lambda: sp.sparge_cache_attn(c, q, other), lambda: sp.sparge_cache_plan(c, new, 5, out=other), lambda: sp.sparge_cache_plan(c, new.long(), 5), lambda: sp.sparge_cache_plan(c, new[:1], 5), lambda: sp.sparge_cache_plan(c, new.cpu(), 5),
              lambda: sp.sparge_cache_plan(c, new, 5, release=new), lambda: sp.sparge_cache_plan(c, new, 4, out=plan),
              lambda: sp.sparge_cache_plan(c, new, -1),
              lambda: sp.sparge_cache_append(c, x[:4], x, plan), lambda: sp.sparge_cache_append(c, x, x.half(), plan),
