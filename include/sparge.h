@@ -316,6 +316,7 @@ typedef struct sparge_cache {
     void *k, *v;                        /* [n_pages, H_kv, 64 d] bytes */
     float *k_amax, *v_amax;             /* [n_pages, H_kv] */
     void *k_tail, *v_tail;              /* 16-bit [R, H_kv, 64, d] */
+    float *k_tail_amax, *v_tail_amax;   /* [R, H_kv, 64]: max |x| of each of those tokens */
     int32_t* table;                     /* [R, max_blocks] */
     int32_t* length;                    /* [R] tokens that row r holds */
     int32_t* free_pages;                /* [n_pages] stack of free pages */

@@ -33,7 +33,7 @@ class _Desc(ctypes.Structure):
 
 class _Cache(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("R", "H_kv", "d", "dtype", "n_pages", "max_blocks")] + [
-        (n, ctypes.c_void_p) for n in ("k", "v", "k_amax", "v_amax", "k_tail", "v_tail", "table", "length", "free_pages",
+        (n, ctypes.c_void_p) for n in ("k", "v", "k_amax", "v_amax", "k_tail", "v_tail", "k_tail_amax", "v_tail_amax", "table", "length", "free_pages",
                                        "n_free", "k_shift")]
 
 
@@ -462,12 +462,14 @@ class SpargeCache:
         self.k, self.v = (empty(n_pages, kv_heads, CACHE_PAGE * head_dim, dt=torch.uint8) for _ in range(2))
         self.k_amax, self.v_amax = (torch.zeros((n_pages, kv_heads), dtype=torch.float32, device=self.device) for _ in range(2))
         self.k_tail, self.v_tail = (empty(rows, kv_heads, CACHE_PAGE, head_dim, dt=dtype) for _ in range(2))
+        self.k_tail_amax, self.v_tail_amax = (empty(rows, kv_heads, CACHE_PAGE, dt=torch.float32) for _ in range(2))
         if k_shift is not None:
             _array(k_shift, torch.float32, (rows, kv_heads, head_dim), self.device, "k_shift")
         self.k_shift = k_shift
         self._struct = _Cache(rows, kv_heads, head_dim, 0 if dtype == torch.float16 else 1, n_pages, max_blocks,
                               *[None if t is None else t.data_ptr() for t in (
-                                  self.k, self.v, self.k_amax, self.v_amax, self.k_tail, self.v_tail, self.table, self.length,
+                                  self.k, self.v, self.k_amax, self.v_amax, self.k_tail, self.v_tail, self.k_tail_amax,
+                                  self.v_tail_amax, self.table, self.length,
                                   self.free_pages, self.n_free, k_shift)])
         self._ref = ctypes.byref(self._struct)
         self._ws_bytes = {}     # query heads -> sparge_cache_attn_workspace_bytes

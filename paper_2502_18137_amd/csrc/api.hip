@@ -962,6 +962,8 @@ int sparge_cache_append(const sparge_cache* cache, const void* K, const void* V,
     if (rc || (rc = check_pages(cache))) return rc;
     if (!cache->k_tail || !cache->v_tail || misaligned(cache->k_tail) || misaligned(cache->v_tail))
         return fail(SPARGE_EINVAL, "k_tail and v_tail must be 16-byte aligned device memory");
+    if (!cache->k_tail_amax || !cache->v_tail_amax || off4(cache->k_tail_amax) || off4(cache->v_tail_amax))
+        return fail(SPARGE_EINVAL, "k_tail_amax and v_tail_amax must be 4-byte aligned device memory");
     if ((rc = check_slots(n_slots))) return rc;
     if (n_slots == 0) return SPARGE_OK;
     if (!K || !V || !cu || !slots || !req) return fail(SPARGE_EINVAL, "NULL argument");

@@ -6,7 +6,7 @@ namespace sparge {
 namespace {
 
 constexpr int PLAN_THREADS = 1024;
-constexpr int FILL_IN_PLAN = 8 * PLAN_THREADS;   // slots that the plan's one workgroup fills itself
+constexpr int FILL_IN_PLAN = 4 * PLAN_THREADS;   // slots that the plan's one workgroup fills itself
 
 __device__ __forceinline__ int blocks_of(int tokens) { return (tokens + PAGE - 1) / PAGE; }
 
@@ -56,6 +56,32 @@ __device__ __forceinline__ void fill_slot(const sparge_cache& c, const int* cu, 
     req[i] = r;
 }
 
+// put(r, a, b, get(r, a, b)) for the n items a of all rows (b: a less the row's first), CH at a time per thread: one search,
+// then along the rows, all loads before the stores
+template <int CH, class Get, class Put>
+__device__ __forceinline__ void deal_out_by(const int* prefix, int rows, int n, Get get, Put put) {
+    for (int a0 = CH * threadIdx.x; a0 < n; a0 += CH * PLAN_THREADS) {
+        int row[CH], value[CH], r = row_of(prefix, rows, a0);
+#pragma unroll
+        for (int e = 0; e < CH; ++e) {
+            const int a = a0 + e;
+            if (a < n) {
+                while (r + 1 < rows && prefix[r + 1] <= a) ++r;
+                row[e] = r;
+                value[e] = get(r, a, a - prefix[r]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < CH; ++e)
+            if (a0 + e < n) put(row[e], a0 + e, a0 + e - prefix[row[e]], value[e]);
+    }
+}
+template <class Get, class Put>
+__device__ __forceinline__ void deal_out(const int* prefix, int rows, int n, Get get, Put put) {
+    if (n <= 2 * PLAN_THREADS) deal_out_by<2>(prefix, rows, n, get, put);
+    else deal_out_by<12>(prefix, rows, n, get, put);   // 8000 pages that change hands: one round trip instead of two
+}
+
 // One workgroup.  Lengths and new tokens are summed over the rows, everything is checked, and only then is anything changed.
 // What bounds it is a chain of four round trips to memory (lengths; the pages that rows give up; the pages that rows take;
 // the table entries that slots are made of), so rows, pages and slots are spread over the threads through the prefix sums.
@@ -76,9 +102,20 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
     int flags = 0;
     const int n_free = c.n_free[0];
     if (n_free < 0 || n_free > c.n_pages) flags = SPARGE_CACHE_BAD_STATE;
-    for (int r = r0; r < r1; ++r) {
-        const int len = c.length[r], n = new_len[r];
-        const bool rel = release && release[r];
+    constexpr int PER = SPARGE_CACHE_MAX_ROWS / PLAN_THREADS;
+    int lens[PER], news[PER];
+    bool rels[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const int r = r0 + e;
+        if (r >= r1) continue;
+        lens[e] = c.length[r], news[e] = new_len[r], rels[e] = release && release[r];
+    }
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        if (r0 + e >= r1) continue;
+        const int len = lens[e], n = news[e];
+        const bool rel = rels[e];
         if (len < 0 || len > most || n < 0) flags |= SPARGE_CACHE_BAD_STATE;
         const long long held = rel ? 0 : len;
         if (held + n > most) flags |= SPARGE_CACHE_ROW_FULL;
@@ -103,34 +140,33 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
         if (tid == 0) status[0] = flags, status[1] = n_free;
         return;
     }
-    for (int r = r0; r < r1; ++r) {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const int r = r0 + e;
+        if (r >= r1) continue;
         push_at[r] = static_cast<int>(at.push), need_at[r] = static_cast<int>(at.need), tok_at[r] = static_cast<int>(at.tok);
         cu[r] = static_cast<int>(at.tok);
-        const int len = c.length[r], n = new_len[r];
-        const bool rel = release && release[r];
-        const int held = rel ? 0 : len;
-        at.push += rel ? blocks_of(len) : 0;
+        const int n = news[e], held = rels[e] ? 0 : lens[e];
+        at.push += rels[e] ? blocks_of(lens[e]) : 0;
         at.need += blocks_of(held + n) - blocks_of(held);
         at.tok += n;
     }
     __syncthreads();
     const int pushed = static_cast<int>(total.push), needed = static_cast<int>(total.need), tokens = static_cast<int>(total.tok);
-    for (int a = tid; a < pushed; a += PLAN_THREADS) {
-        const int r = row_of(push_at, c.R, a);
-        c.free_pages[n_free + a] = c.table[static_cast<long long>(r) * c.max_blocks + a - push_at[r]];
+    int32_t* stack = c.free_pages + n_free;
+    auto entry = [&](int r, int b) -> int32_t& { return c.table[static_cast<long long>(r) * c.max_blocks + b]; };
+    deal_out(push_at, c.R, pushed, [&](int r, int a, int b) { return entry(r, b); }, [&](int r, int a, int b, int page) { stack[a] = page; });
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        if (r0 + e >= r1) continue;
+        const int held = rels[e] ? 0 : lens[e];
+        push_at[r0 + e] = held;
+        c.length[r0 + e] = held + news[e];
     }
     __syncthreads();
-    for (int r = r0; r < r1; ++r) {
-        const int held = release && release[r] ? 0 : c.length[r];
-        push_at[r] = held;
-        c.length[r] = held + new_len[r];
-    }
-    __syncthreads();
-    for (int a = tid; a < needed; a += PLAN_THREADS) {
-        const int r = row_of(need_at, c.R, a);
-        c.table[static_cast<long long>(r) * c.max_blocks + blocks_of(push_at[r]) + a - need_at[r]] =
-            c.free_pages[n_free + pushed - 1 - a];
-    }
+    deal_out(need_at, c.R, needed, [&](int r, int a, int b) { return stack[pushed - 1 - a]; },
+             [&](int r, int a, int b, int page) { entry(r, blocks_of(push_at[r]) + b) = page; });
     if (tid == 0) {
         cu[c.R] = tokens;
         c.n_free[0] = n_free + pushed - needed;
@@ -141,8 +177,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
     for (int i = tid; i < n_slots; i += PLAN_THREADS) fill_slot(c, tok_at, tokens, i, push_at, slots, req);
 }
 
-// The slot map of a long step, from what the plan has written; a workgroup per 2048 slots.
-constexpr int FILL_SLOTS = 2048;
+// The slot map of a long step, from what the plan has written; a workgroup per 512 slots.
+constexpr int FILL_SLOTS = 512;
 __global__ __launch_bounds__(256) void cache_slots_kernel(sparge_cache c, int n_slots, const int32_t* __restrict__ cu,
                                                           int32_t* slots, int32_t* req) {
     extern __shared__ int lds[];
@@ -172,27 +208,54 @@ __device__ __forceinline__ int code_of(float x, int up, float amax1, float r) {
     return i + ((over > 0.f || (over == 0.f && (i & 1))) ? 1 : 0);
 }
 
-// A workgroup quantizes one kv head's K or V of every page that begins to get tokens inside its window of `window` (a power of two up to
-// 64) slots: the open page's older tokens from the tail, the new ones from the call's tensor.  The amax is taken over the
-// bit patterns, so that a NaN or an infinity is the largest.  The row's first page also stores the tokens of the row's last
-// page if that stays open (after it has read the older ones, which lie in the same place).
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }   // a NaN or an infinity is the largest
+
+// What the codes of a block with this amax are made with; codes are 0 in a block of zeros or with an infinity or a NaN.
+struct Quantizer {
+    bool plain;
+    int up;
+    float amax1, inv;
+
+    __device__ explicit Quantizer(uint32_t top) {
+        const float amax = __uint_as_float(top);
+        plain = top > 0 && top < 0x7F800000u;
+        up = plain ? 1 - __builtin_amdgcn_frexp_expf(amax) : 1;
+        amax1 = plain ? __builtin_ldexpf(amax, up) : 1.0f, inv = 127.0f / amax1;
+    }
+    __device__ __forceinline__ uint32_t byte(float x) const { return static_cast<uint32_t>((plain ? code_of(x, up, amax1, inv) : 0) + 128); }
+};
+
+// the largest of 256 threads' values; lds: 4
+__device__ __forceinline__ uint32_t workgroup_max(uint32_t v, uint32_t* lds) {
+    for (int s = 1; s < 64; s <<= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), s)));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return max(max(lds[0], lds[1]), max(lds[2], lds[3]));
+}
+
+// A workgroup quantizes one kv head's K or V of every page that begins to get tokens inside its window of `window` (a power of two
+// up to 64) slots: the open page's older tokens from the tail, the new ones from the call's tensor.  Bound by its bytes: a
+// thread holds what makes whole 16-byte pieces of the page (K: 16 channels of a token; V: a channel of 16 tokens), loads and
+// stores are coalesced and nothing goes through LDS but the maxima.  Where a page gets few tokens that do not raise its amax
+// (decoding: all but one of t + 1 at the t-th token of a page), the older codes are what they were and only the new ones are
+// written; the tail's amax per token tells without reading the tail.
+// The row's first page also stores the tokens of the row's last page if that stays open (after it has read the older
+// ones, which lie in the same place).
+constexpr int FEW = 8;   // tokens of a page whose codes are written by themselves
 template <int D, int DT>
-__global__ __launch_bounds__(256) void cache_append_kernel(sparge_cache c, const uint16_t* __restrict__ K,
+__global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, const uint16_t* __restrict__ K,
                                                            const uint16_t* __restrict__ V, int n_slots, int window, long long k_sn,
                                                            long long k_sh, long long v_sn, long long v_sh,
                                                            const int32_t* __restrict__ cu, const int32_t* __restrict__ slots,
                                                            const int32_t* __restrict__ req) {
-    constexpr int LPR = D / 8, RPS = 256 / LPR, NL = PAGE / RPS;   // lanes per row, rows a step, steps
-    __shared__ __align__(16) uint8_t codes[PAGE * D];
-    __shared__ uint32_t wave_amax[4];
-    const int tid = threadIdx.x, lane = tid & 63, hk = blockIdx.y;
+    constexpr int LPR = D / 8, RPS = 256 / LPR;   // threads per token of 8 channels each, tokens at a time
+    constexpr int CV = D / 64;                    // V: channels per thread; K: pieces per thread
+    __shared__ uint32_t lds_max[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hk = blockIdx.y;
     const bool is_v = blockIdx.z != 0;
     const uint16_t* x = is_v ? V + hk * v_sh : K + hk * k_sh;
     const long long sn = is_v ? v_sn : k_sn;
-    uint16_t* tails = static_cast<uint16_t*>(is_v ? c.v_tail : c.k_tail);
-    uint8_t* pages = static_cast<uint8_t*>(is_v ? c.v : c.k);
-    float* amaxes = is_v ? c.v_amax : c.k_amax;
-    const float* shifts = is_v ? nullptr : c.k_shift;
 
     const int i0 = blockIdx.x * window;
     int my_slot = -1, my_row = -1, my_prev = -1;
@@ -203,7 +266,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(sparge_cache c, const
     }
     const bool there = my_slot >= 0 && my_slot / PAGE < c.n_pages && my_row >= 0 && my_row < c.R;
     unsigned long long starts = __ballot(there && (my_slot % PAGE == 0 || my_prev != my_row));
-    const int col = (tid % LPR) * 8, row0 = tid / LPR;
+    const int col = (tid % LPR) * 8, tok = tid / LPR;   // where 8 channels of a token are taken
     while (starts) {
         const int first = __builtin_ctzll(starts);
         starts &= starts - 1;
@@ -212,115 +275,218 @@ __global__ __launch_bounds__(256) void cache_append_kernel(sparge_cache c, const
         const int page = slot / PAGE, off = slot % PAGE;
         const int row_begin = max(0, min(cu[r], n_slots)), row_end = max(0, min(cu[r + 1], n_slots));
         const int n = max(1, min(PAGE - off, row_end - i));
-        uint16_t* tail = tails + (static_cast<long long>(r) * c.H_kv + hk) * PAGE * D;
-        float y[NL][8];
-        uint32_t top = 0;
-#pragma unroll
-        for (int s = 0; s < NL; ++s) {
-            const int t = s * RPS + row0;
-            uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-            if (t < off) raw = *reinterpret_cast<const uint4*>(tail + t * D + col);
-            else if (t < off + n) raw = *reinterpret_cast<const uint4*>(x + (i + t - off) * sn + col);
+        const long long at = static_cast<long long>(page) * c.H_kv + hk, row_at = static_cast<long long>(r) * c.H_kv + hk;
+        uint16_t* tail = static_cast<uint16_t*>(is_v ? c.v_tail : c.k_tail) + row_at * PAGE * D;
+        float* tail_amax = (is_v ? c.v_tail_amax : c.k_tail_amax) + row_at * PAGE;
+        const float* shift = is_v || !c.k_shift ? nullptr : c.k_shift + row_at * D;
+        uint8_t* codes = static_cast<uint8_t*>(is_v ? c.v : c.k) + at * PAGE * D;
+        auto load8 = [&](const uint16_t* p, float (&y)[8]) {
+            const uint4 raw = *reinterpret_cast<const uint4*>(p);
             const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[s][2 * e] = cvt16<DT>(static_cast<uint16_t>(w[e] & 0xFFFFu));
-                y[s][2 * e + 1] = cvt16<DT>(static_cast<uint16_t>(w[e] >> 16));
+            for (int e = 0; e < 8; ++e) y[e] = cvt16<DT>(static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)))) - (shift ? shift[col + e] : 0.f);
+            return raw;
+        };
+        bool done = false;
+        if (n <= FEW) {
+            float y[8] = {};
+            uint32_t top = 0;
+            const uint32_t before = tid < off ? __float_as_uint(tail_amax[tid]) : 0u;
+            if (tok < n) {
+                load8(x + (i + tok) * sn + col, y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = max(top, abs_bits(y[e]));
+            }
+            const uint32_t old = workgroup_max(before, lds_max), now = workgroup_max(top, lds_max);
+            if (off == 0 || old >= now) {
+                done = true;
+                const uint32_t amax = max(old, now);
+                const Quantizer q(amax);
+                if (tok < n) {
+                    uint32_t b[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) b[e] = q.byte(y[e]);
+                    if (is_v) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) codes[v_byte(off + tok, col + e)] = static_cast<uint8_t>(b[e]);
+                    } else {
+                        *reinterpret_cast<uint2*>(codes + k_byte(off + tok, col, D)) =
+                            make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+                    }
+                }
+                if (tid == 0) (is_v ? c.v_amax : c.k_amax)[at] = __uint_as_float(amax);
             }
         }
-        if (shifts) {
-            const float* sh = shifts + (static_cast<long long>(r) * c.H_kv + hk) * D + col;
+        if (!done) {
+            // K: pieces wave + 4 p: token 16 (piece / CV) + lane % 16, channels 64 (piece % CV) + 16 (lane / 16) + 0..15
+            // V: tokens 16 t + 4 wave + 0..3, channels CV lane + 0..CV-1
+            // (kept as they come, 16 bits each: twice the workgroups fit a compute unit)
+            uint32_t raw[CV][8];
+            auto k_token = [&](int p) { return 16 * ((wave + 4 * p) / CV) + (lane & 15); };
+            auto k_channel = [&](int p) { return 64 * ((wave + 4 * p) % CV) + 16 * (lane >> 4); };
+            if (is_v) {
+                uint32_t w[16];
 #pragma unroll
-            for (int s = 0; s < NL; ++s)
-                if (s * RPS + row0 < off + n)
+                for (int e = 0; e < 16; ++e) {
+                    const int t = 16 * (e >> 2) + 4 * wave + (e & 3);
+                    const uint16_t* from = (t < off ? tail + t * D : x + (i + t - off) * sn) + CV * lane;
+                    w[e] = 0;
+                    if (t < off + n) {
+                        if constexpr (CV == 2) w[e] = *reinterpret_cast<const uint32_t*>(from); else w[e] = *from;
+                    }
+                }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[s][e] -= sh[e];
-        }
+                for (int p = 0; p < CV; ++p)
 #pragma unroll
-        for (int s = 0; s < NL; ++s)
+                    for (int e = 0; e < 8; ++e)   // the 16-bit halves p of two words side by side
+                        raw[p][e] = __builtin_amdgcn_perm(w[2 * e + 1], w[2 * e], p ? 0x07060302u : 0x05040100u);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(y[s][e]) & 0x7FFFFFFFu);
-        for (int s = 1; s < 64; s <<= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), s)));
-        if (lane == 0) wave_amax[tid >> 6] = top;
-        __syncthreads();   // (the tail's older tokens are read, too)
-        top = max(max(wave_amax[0], wave_amax[1]), max(wave_amax[2], wave_amax[3]));
-        const bool plain = top > 0 && top < 0x7F800000u;   // a block with an infinity or a NaN has codes 0
-        int up = 1;
-        const float amax = __uint_as_float(top);
-        if (plain) up = 1 - __builtin_amdgcn_frexp_expf(amax);
-        const float amax1 = plain ? __builtin_ldexpf(amax, up) : 1.0f, inv = 127.0f / amax1;
-#pragma unroll
-        for (int s = 0; s < NL; ++s) {
-            const int t = s * RPS + row0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int code = plain ? code_of(y[s][e], up, amax1, inv) : 0;
-                codes[is_v ? v_byte(t, col + e) : k_byte(t, col + e, D)] = static_cast<uint8_t>(code + 128);
+                for (int p = 0; p < CV; ++p) {
+                    const int t = k_token(p);
+                    uint4 two[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+                    const uint4* from = reinterpret_cast<const uint4*>((t < off ? tail + t * D : x + (i + t - off) * sn) + k_channel(p));
+                    if (t < off + n) two[0] = from[0], two[1] = from[1];
+                    __builtin_memcpy(raw[p], two, 32);
+                }
             }
+            auto value = [&](int p, int e) {
+                const float y = cvt16<DT>(static_cast<uint16_t>(raw[p][e >> 1] >> (16 * (e & 1))));
+                return shift && k_token(p) < off + n ? y - shift[k_channel(p) + e] : y;
+            };
+            uint32_t top = 0;
+#pragma unroll
+            for (int p = 0; p < CV; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = max(top, abs_bits(value(p, e)));
+            top = workgroup_max(top, lds_max);
+            const Quantizer q(top);
+#pragma unroll
+            for (int p = 0; p < CV; ++p)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(raw[p][e]));   // unpacked again, not kept as fp32 from the maximum on
+#pragma unroll
+            for (int p = 0; p < CV; ++p) {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    w[e] = q.byte(value(p, 4 * e)) | q.byte(value(p, 4 * e + 1)) << 8 | q.byte(value(p, 4 * e + 2)) << 16 | q.byte(value(p, 4 * e + 3)) << 24;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                const int ch = CV * lane + p;
+                const int piece = is_v ? (ch >> 4) * 64 + (ch & 15) + 16 * wave : (wave + 4 * p) * 64 + lane;
+                reinterpret_cast<uint4*>(codes)[piece] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            if (tid == 0) (is_v ? c.v_amax : c.k_amax)[at] = __uint_as_float(top);
         }
-        if (i == row_begin) {   // the tokens of the row's last page, if it stays open
+        if (i == row_begin) {   // the tokens of the row's last page, if it stays open (the older ones have been read: the maxima's barriers)
             const int last = row_end > 0 ? slots[row_end - 1] : -1;
             const int open = last >= 0 ? (last % PAGE + 1) % PAGE : 0;
             const int keep = min(open, row_end - row_begin);
-            for (int t = open - keep + row0; t < open; t += RPS)
-                *reinterpret_cast<uint4*>(tail + t * D + col) = *reinterpret_cast<const uint4*>(x + (row_end - open + t) * sn + col);
+            for (int t = open - keep + tok; t < open; t += RPS) {
+                float y[8];
+                const uint4 raw = load8(x + (row_end - open + t) * sn + col, y);
+                uint32_t top = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = max(top, abs_bits(y[e]));
+#pragma unroll
+                for (int s = 1; s < LPR; s <<= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), s)));
+                *reinterpret_cast<uint4*>(tail + t * D + col) = raw;
+                if (col == 0) tail_amax[t] = __uint_as_float(top);
+            }
         }
-        __syncthreads();
-        const long long at = static_cast<long long>(page) * c.H_kv + hk;
-        for (int b = tid; b < PAGE * D / 16; b += 256)
-            reinterpret_cast<uint4*>(pages + at * PAGE * D)[b] = reinterpret_cast<const uint4*>(codes)[b];
-        if (tid == 0) amaxes[at] = amax;
-        __syncthreads();   // the next page uses the LDS again
     }
 }
 
 // ---- read-back ---------------------------------------------------------------------------------------------------
 
-// value = code amax / 127 (+ shift), in 64 bits and rounded once to fp32, then to 16 bits where asked for.  A thread gives 16
-// channels of one token of one kv head, K (blockIdx.z 0) or V.
-template <int D, int OUT>
-__global__ __launch_bounds__(256) void cache_read_kernel(sparge_cache c, const int32_t* __restrict__ slots,
-                                                         const int32_t* __restrict__ req, int n_slots, void* K, void* V) {
-    constexpr int TPT = D / 16, TOK = 256 / TPT;   // threads per token, tokens per workgroup
-    const int hk = blockIdx.y, i = blockIdx.x * TOK + threadIdx.x / TPT, ch = (threadIdx.x % TPT) * 16;
-    const bool is_v = blockIdx.z != 0;
-    if (i >= n_slots) return;
-    const int slot = slots[i], r = req ? req[i] : 0;
-    if (slot < 0 || slot / PAGE >= c.n_pages || r < 0 || r >= c.R) return;
-    const int page = slot / PAGE, key = slot % PAGE;
-    const long long at = static_cast<long long>(page) * c.H_kv + hk;
-    const uint8_t* p = static_cast<const uint8_t*>(is_v ? c.v : c.k) + at * PAGE * D;
-    uint8_t b[16];
-    if (is_v) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) b[e] = p[v_byte(key, ch + e)];
-    } else {
-        const uint4 w = *reinterpret_cast<const uint4*>(p + k_byte(key, ch, D));
-        __builtin_memcpy(b, &w, 16);
-    }
-    const double step = static_cast<double>((is_v ? c.v_amax : c.k_amax)[at]) / 127.0;
-    const float* sh = !is_v && c.k_shift ? c.k_shift + (static_cast<long long>(r) * c.H_kv + hk) * D + ch : nullptr;
-    float y[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        double v = static_cast<double>(static_cast<int>(b[e]) - 128) * step;
-        if (sh) v += static_cast<double>(sh[e]);
-        y[e] = static_cast<float>(v);
-    }
-    const long long o = (static_cast<long long>(i) * c.H_kv + hk) * D + ch;
-    void* out = is_v ? V : K;
+// value = code amax / 127 (+ shift), in 64 bits and rounded once to fp32, then to 16 bits where asked for.  A workgroup takes the
+// runs of consecutive slots of one page inside its window of `window` (a power of two up to 64) slots, K (blockIdx.z 0) or V
+// of one kv head, from the page's 16-byte pieces as they lie: K a token's 16 channels, V a channel of 16 tokens, whose
+// neighbours write the tokens' neighbouring channels.
+template <int OUT>
+__device__ __forceinline__ void put(void* out, long long at, const float* y, int n) {   // n = 1, 2 or a multiple of 4 (8) values
     if constexpr (OUT == SPARGE_F32) {
-#pragma unroll
-        for (int e = 0; e < 16; e += 4)
-            *reinterpret_cast<float4*>(static_cast<float*>(out) + o + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+        float* p = static_cast<float*>(out) + at;
+        if (n == 1) *p = y[0];
+        else if (n == 2) *reinterpret_cast<float2*>(p) = make_float2(y[0], y[1]);
+        else for (int e = 0; e < n; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
     } else {
-        uint16_t h[16];
+        uint16_t* p = static_cast<uint16_t*>(out) + at;
+        if (n == 1) *p = cvt_to16<OUT>(y[0]);
+        else if (n == 2) *reinterpret_cast<uint32_t*>(p) = cvt_to16<OUT>(y[0]) | static_cast<uint32_t>(cvt_to16<OUT>(y[1])) << 16;
+        else for (int e = 0; e < n; e += 8) {
+            uint32_t w[4];
+            for (int k = 0; k < 4; ++k) w[k] = cvt_to16<OUT>(y[e + 2 * k]) | static_cast<uint32_t>(cvt_to16<OUT>(y[e + 2 * k + 1])) << 16;
+            *reinterpret_cast<uint4*>(p + e) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+template <int D, int OUT>
+__global__ __launch_bounds__(256, 6) void cache_read_kernel(sparge_cache c, const int32_t* __restrict__ slots,
+                                                         const int32_t* __restrict__ req, int n_slots, int window, void* K, void* V) {
+    constexpr int CV = D / 64;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), hk = blockIdx.y, i0 = blockIdx.x * window;
+    const bool is_v = blockIdx.z != 0;
+    int my_slot = -1, my_row = 0;
+    if (lane < window && i0 + lane < n_slots) {
+        my_slot = slots[i0 + lane];
+        if (req) my_row = req[i0 + lane];
+    }
+    const bool there = my_slot >= 0 && my_slot / PAGE < c.n_pages && my_row >= 0 && my_row < c.R;
+    const int prev_slot = __shfl_up(my_slot, 1), prev_row = __shfl_up(my_row, 1);
+    const bool goes_on = there && lane > 0 && my_slot == prev_slot + 1 && my_slot % PAGE != 0 && my_row == prev_row;
+    unsigned long long starts = __ballot(there && !goes_on);
+    const unsigned long long breaks = __ballot(!goes_on);
+    while (starts) {
+        const int first = __builtin_ctzll(starts);
+        starts &= starts - 1;
+        const unsigned long long behind = first == 63 ? 0ull : breaks >> (first + 1);
+        const int n = behind ? __builtin_ctzll(behind) + 1 : 64 - first;   // lanes beyond the window break the run
+        const int slot = __builtin_amdgcn_readlane(my_slot, first), r = __builtin_amdgcn_readlane(my_row, first);
+        const int page = slot / PAGE, off = slot % PAGE;
+        const long long at = static_cast<long long>(page) * c.H_kv + hk;
+        const uint4* codes = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(is_v ? c.v : c.k) + at * PAGE * D);
+        const double step = static_cast<double>((is_v ? c.v_amax : c.k_amax)[at]) / 127.0;
+        const long long out0 = (static_cast<long long>(i0 + first - off) * c.H_kv + hk) * D;   // of the page's token 0
+        auto value = [&](const uint32_t (&w)[4], int e) {
+            return static_cast<double>(static_cast<int>((w[e >> 2] >> (8 * (e & 3))) & 0xFFu) - 128) * step;
+        };
+        if (is_v) {
+            uint32_t w[CV][4];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) h[e] = cvt_to16<OUT>(y[e]);
-        uint4 w[2];
-        __builtin_memcpy(w, h, 32);
-        reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + o)[0] = w[0];
-        reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + o)[1] = w[1];
+            for (int p = 0; p < CV; ++p) {
+                const int ch = CV * lane + p;
+                const uint4 raw = codes[(ch >> 4) * 64 + (ch & 15) + 16 * wave];
+                w[p][0] = raw.x, w[p][1] = raw.y, w[p][2] = raw.z, w[p][3] = raw.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int t = 16 * (e >> 2) + 4 * wave + (e & 3);
+                if (t < off || t >= off + n) continue;
+                float y[CV];
+#pragma unroll
+                for (int p = 0; p < CV; ++p) y[p] = static_cast<float>(value(w[p], e));
+                put<OUT>(V, out0 + static_cast<long long>(t) * c.H_kv * D + CV * lane, y, CV);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            const float* shift = c.k_shift ? c.k_shift + (static_cast<long long>(r) * c.H_kv + hk) * D : nullptr;
+#pragma unroll
+            for (int p = 0; p < CV; ++p) {
+                const int piece = wave + 4 * p, t = 16 * (piece / CV) + (lane & 15), ch = 64 * (piece % CV) + 16 * (lane >> 4);
+                if (t < off || t >= off + n) continue;
+                const uint4 raw = codes[piece * 64 + lane];
+                const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+                float y[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    y[e] = static_cast<float>(shift ? value(w, e) + static_cast<double>(shift[ch + e]) : value(w, e));
+                    if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+                put<OUT>(K, out0 + static_cast<long long>(t) * c.H_kv * D + ch, y, 16);
+            }
+        }
     }
 }
 
@@ -336,13 +502,18 @@ hipError_t launch_cache_plan(const sparge_cache& c, const int32_t* new_len, cons
     return hipGetLastError();
 }
 
+// Slots per workgroup of the append and the read-back: a page's worth where there are that many, down to one (which may be a page
+// of its own) where there are few: a workgroup takes its window's pages one after the other.
+static int window_of(int n_slots, int heads) {
+    int window = 64;
+    while (window > 1 && static_cast<long long>(n_slots / window) * heads < 512) window /= 2;
+    return window;
+}
+
 hipError_t launch_cache_append(const sparge_cache& c, const void* K, const void* V, int n_slots, long long k_sn, long long k_sh,
                                long long v_sn, long long v_sh, const int32_t* cu, const int32_t* slots, const int32_t* req,
                                hipStream_t st) {
-    // a window per page where a step has that many, down to one per slot (each of which may be a page of its own) where there
-    // are few: a workgroup quantizes its window's pages one after the other
-    int window = 64;
-    while (window > 1 && static_cast<long long>(n_slots / window) * c.H_kv < 4096) window /= 2;
+    const int window = window_of(n_slots, c.H_kv);
     const dim3 grid((n_slots + window - 1) / window, c.H_kv, 2);
     const uint16_t *k = static_cast<const uint16_t*>(K), *v = static_cast<const uint16_t*>(V);
 #define APPEND(D, DT) \
@@ -358,9 +529,9 @@ hipError_t launch_cache_append(const sparge_cache& c, const void* K, const void*
 
 hipError_t launch_cache_read(const sparge_cache& c, const int32_t* slots, const int32_t* req, int n_slots, int out_dtype, void* K,
                              void* V, hipStream_t st) {
-    const int tok = 256 / (c.d / 16);
-    const dim3 grid((n_slots + tok - 1) / tok, c.H_kv, 2);
-#define READ(D, OUT) hipLaunchKernelGGL((cache_read_kernel<D, OUT>), grid, dim3(256), 0, st, c, slots, req, n_slots, K, V)
+    const int window = window_of(n_slots, c.H_kv);
+    const dim3 grid((n_slots + window - 1) / window, c.H_kv, 2);
+#define READ(D, OUT) hipLaunchKernelGGL((cache_read_kernel<D, OUT>), grid, dim3(256), 0, st, c, slots, req, n_slots, window, K, V)
     if (c.d == 64) {
         if (out_dtype == SPARGE_F32) READ(64, SPARGE_F32); else if (out_dtype == SPARGE_F16) READ(64, SPARGE_F16); else READ(64, SPARGE_BF16);
     } else {

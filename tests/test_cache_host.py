@@ -74,7 +74,7 @@ def lib():
 
 def cache(**kw):
     from paper_2502_18137_amd.binding import _Cache
-    f = dict(R=2, H_kv=2, d=64, dtype=1, n_pages=10, max_blocks=4, k=P, v=P, k_amax=P, v_amax=P, k_tail=P, v_tail=P, table=P, length=P,
+    f = dict(R=2, H_kv=2, d=64, dtype=1, n_pages=10, max_blocks=4, k=P, v=P, k_amax=P, v_amax=P, k_tail=P, v_tail=P, k_tail_amax=P, v_tail_amax=P, table=P, length=P,
              free_pages=P, n_free=P, k_shift=0)
     f.update(kw)
     return ctypes.byref(_Cache(**f))
@@ -124,7 +124,7 @@ def test_pointers_that_are_refused(lib):
     for f in (append, read, attn):
         for kw, want in BAD_PAGES:
             refused(f(lib, cache(**kw)), want, lib)
-    for kw in (dict(k_tail=0), dict(v_tail=0), dict(k_tail=P + 8), dict(v_tail=P + 4)):
+    for kw in (dict(k_tail=0), dict(v_tail=0), dict(k_tail=P + 8), dict(v_tail=P + 4), dict(k_tail_amax=0), dict(v_tail_amax=0), dict(k_tail_amax=P + 2)):
         refused(append(lib, cache(**kw)), -1, lib)
     for kw in (dict(K=0), dict(V=0), dict(K=P + 8), dict(V=P + 2), dict(cu=0), dict(slots=0), dict(req=0), dict(slots=P + 2),
                dict(s=(-8, 64, 128, 64)), dict(s=(128, 64, 128, 60)), dict(s=(128, 64, 100, 64))):
