@@ -26,22 +26,30 @@ struct Sums {
 };
 
 // exclusive prefix of v over the workgroup's threads, and the total; lds: a Sums per wave
-__device__ Sums scan(Sums v, Sums* lds, Sums& total) {
+__device__ __forceinline__ Sums up(const Sums& v, int lanes, int width) {
+    return {__shfl_up(v.push, lanes, width), __shfl_up(v.need, lanes, width), __shfl_up(v.tok, lanes, width)};
+}
+__device__ Sums scan(const Sums& v, Sums* lds, Sums& total) {
+    constexpr int WAVES = PLAN_THREADS / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Sums x = v;
+#pragma unroll 1
     for (int s = 1; s < 64; s <<= 1) {
-        const long long a = __shfl_up(x.push, s), b = __shfl_up(x.need, s), c = __shfl_up(x.tok, s);
-        if (lane >= s) x.push += a, x.need += b, x.tok += c;
+        const Sums y = up(x, s, 64);
+        if (lane >= s) x.push += y.push, x.need += y.need, x.tok += y.tok;
     }
     if (lane == 63) lds[wave] = x;
     __syncthreads();
-    Sums before = {0, 0, 0};
-    total = {0, 0, 0};
-    for (int w = 0; w < PLAN_THREADS / 64; ++w) {
-        if (w == wave) before = total;
-        total.push += lds[w].push, total.need += lds[w].need, total.tok += lds[w].tok;
+    Sums w = lds[lane % WAVES];
+#pragma unroll 1
+    for (int s = 1; s < WAVES; s <<= 1) {
+        const Sums y = up(w, s, WAVES);
+        if (lane % WAVES >= s) w.push += y.push, w.need += y.need, w.tok += y.tok;
     }
-    return {before.push + x.push - v.push, before.need + x.need - v.need, before.tok + x.tok - v.tok};
+    total = {__shfl(w.push, WAVES - 1), __shfl(w.need, WAVES - 1), __shfl(w.tok, WAVES - 1)};
+    const Sums before = {__shfl(w.push, max(wave - 1, 0)), __shfl(w.need, max(wave - 1, 0)), __shfl(w.tok, max(wave - 1, 0))};
+    if (wave) x.push += before.push, x.need += before.need, x.tok += before.tok;
+    return {x.push - v.push, x.need - v.need, x.tok - v.tok};
 }
 
 __device__ __forceinline__ void fill_slot(const sparge_cache& c, const int* cu, int total, int i, const int* held, int32_t* slots,
@@ -56,35 +64,11 @@ __device__ __forceinline__ void fill_slot(const sparge_cache& c, const int* cu, 
     req[i] = r;
 }
 
-// put(r, a, b, get(r, a, b)) for the n items a of all rows (b: a less the row's first), CH at a time per thread: one search,
-// then along the rows, all loads before the stores
-template <int CH, class Get, class Put>
-__device__ __forceinline__ void deal_out_by(const int* prefix, int rows, int n, Get get, Put put) {
-    for (int a0 = CH * threadIdx.x; a0 < n; a0 += CH * PLAN_THREADS) {
-        int row[CH], value[CH], r = row_of(prefix, rows, a0);
-#pragma unroll
-        for (int e = 0; e < CH; ++e) {
-            const int a = a0 + e;
-            if (a < n) {
-                while (r + 1 < rows && prefix[r + 1] <= a) ++r;
-                row[e] = r;
-                value[e] = get(r, a, a - prefix[r]);
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < CH; ++e)
-            if (a0 + e < n) put(row[e], a0 + e, a0 + e - prefix[row[e]], value[e]);
-    }
-}
-template <class Get, class Put>
-__device__ __forceinline__ void deal_out(const int* prefix, int rows, int n, Get get, Put put) {
-    if (n <= 2 * PLAN_THREADS) deal_out_by<2>(prefix, rows, n, get, put);
-    else deal_out_by<12>(prefix, rows, n, get, put);   // 8000 pages that change hands: one round trip instead of two
-}
-
 // One workgroup.  Lengths and new tokens are summed over the rows, everything is checked, and only then is anything changed.
 // What bounds it is a chain of four round trips to memory (lengths; the pages that rows give up; the pages that rows take;
-// the table entries that slots are made of), so rows, pages and slots are spread over the threads through the prefix sums.
+// the table entries that slots are made of), so rows, pages and slots are spread over the threads through the prefix sums,
+// and the instructions that it runs once: loops that are short anyway stay rolled up (unrolled, with the rows kept in
+// registers, 11 us in the place of 6 for 48 rows).
 __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c, const int32_t* __restrict__ new_len,
                                                                   const uint8_t* __restrict__ release, int n_slots, int32_t* cu,
                                                                   int32_t* slots, int32_t* req, int32_t* status) {
@@ -93,29 +77,20 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
     int* need_at = lds + c.R;
     int* tok_at = lds + 2 * c.R;
     __shared__ Sums wave_sums[PLAN_THREADS / 64];
-    __shared__ int wave_flags[PLAN_THREADS / 64];
+    __shared__ int all_flags;
     const int tid = threadIdx.x;
     const int per = (c.R + PLAN_THREADS - 1) / PLAN_THREADS;
     const int r0 = tid * per, r1 = min(r0 + per, c.R);
     const long long most = static_cast<long long>(c.max_blocks) * PAGE;
+    if (tid == 0) all_flags = 0;
     Sums mine = {0, 0, 0};
     int flags = 0;
     const int n_free = c.n_free[0];
     if (n_free < 0 || n_free > c.n_pages) flags = SPARGE_CACHE_BAD_STATE;
-    constexpr int PER = SPARGE_CACHE_MAX_ROWS / PLAN_THREADS;
-    int lens[PER], news[PER];
-    bool rels[PER];
-#pragma unroll
-    for (int e = 0; e < PER; ++e) {
-        const int r = r0 + e;
-        if (r >= r1) continue;
-        lens[e] = c.length[r], news[e] = new_len[r], rels[e] = release && release[r];
-    }
-#pragma unroll
-    for (int e = 0; e < PER; ++e) {
-        if (r0 + e >= r1) continue;
-        const int len = lens[e], n = news[e];
-        const bool rel = rels[e];
+#pragma unroll 1
+    for (int r = r0; r < r1; ++r) {
+        const int len = c.length[r], n = new_len[r];
+        const bool rel = release && release[r];
         if (len < 0 || len > most || n < 0) flags |= SPARGE_CACHE_BAD_STATE;
         const long long held = rel ? 0 : len;
         if (held + n > most) flags |= SPARGE_CACHE_ROW_FULL;
@@ -124,11 +99,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
         mine.tok += n;
     }
     Sums total;
-    Sums at = scan(mine, wave_sums, total);
-    for (int s = 1; s < 64; s <<= 1) flags |= __shfl_xor(flags, s);
-    if ((tid & 63) == 0) wave_flags[tid >> 6] = flags;
+    Sums at = scan(mine, wave_sums, total);   // (its barrier: all_flags is 0)
+    if (flags) atomicOr(&all_flags, flags);
     __syncthreads();
-    for (int w = 0; w < PLAN_THREADS / 64; ++w) flags |= wave_flags[w];
+    flags = all_flags;
     if (n_free + total.push > c.n_pages) flags |= SPARGE_CACHE_BAD_STATE;
     if (n_free + total.push < total.need) flags |= SPARGE_CACHE_NO_PAGES;
     if (total.tok > n_slots) flags |= SPARGE_CACHE_NO_SLOTS;
@@ -140,33 +114,53 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
         if (tid == 0) status[0] = flags, status[1] = n_free;
         return;
     }
-#pragma unroll
-    for (int e = 0; e < PER; ++e) {
-        const int r = r0 + e;
-        if (r >= r1) continue;
+#pragma unroll 1
+    for (int r = r0; r < r1; ++r) {
         push_at[r] = static_cast<int>(at.push), need_at[r] = static_cast<int>(at.need), tok_at[r] = static_cast<int>(at.tok);
         cu[r] = static_cast<int>(at.tok);
-        const int n = news[e], held = rels[e] ? 0 : lens[e];
-        at.push += rels[e] ? blocks_of(lens[e]) : 0;
+        const int len = c.length[r], n = new_len[r];
+        const bool rel = release && release[r];
+        const int held = rel ? 0 : len;
+        at.push += rel ? blocks_of(len) : 0;
         at.need += blocks_of(held + n) - blocks_of(held);
         at.tok += n;
     }
     __syncthreads();
     const int pushed = static_cast<int>(total.push), needed = static_cast<int>(total.need), tokens = static_cast<int>(total.tok);
     int32_t* stack = c.free_pages + n_free;
-    auto entry = [&](int r, int b) -> int32_t& { return c.table[static_cast<long long>(r) * c.max_blocks + b]; };
-    deal_out(push_at, c.R, pushed, [&](int r, int a, int b) { return entry(r, b); }, [&](int r, int a, int b, int page) { stack[a] = page; });
-    __syncthreads();
+#pragma unroll 1
+    for (int pop = 0; pop < 2; ++pop) {
+        // page a of all that change hands is number a - prefix[r] of row r's; four a thread, one search, then along the rows,
+        // all loads before the stores
+        const int* prefix = pop ? need_at : push_at;
+        const int n = pop ? needed : pushed;
+#pragma unroll 1
+        for (int a0 = 4 * tid; a0 < n; a0 += 4 * PLAN_THREADS) {
+            int r = row_of(prefix, c.R, a0), page[4];
+            int32_t* to[4];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-        if (r0 + e >= r1) continue;
-        const int held = rels[e] ? 0 : lens[e];
-        push_at[r0 + e] = held;
-        c.length[r0 + e] = held + news[e];
+            for (int e = 0; e < 4; ++e) {
+                const int a = min(a0 + e, n - 1);
+                while (r + 1 < c.R && prefix[r + 1] <= a) ++r;
+                const int b = a - prefix[r] + (pop ? blocks_of(push_at[r]) : 0);
+                int32_t* entry = c.table + static_cast<long long>(r) * c.max_blocks + b;
+                int32_t* place = stack + (pop ? pushed - 1 - a : a);
+                to[e] = pop ? entry : place;
+                page[e] = *(pop ? place : entry);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) *to[e] = page[e];   // (beyond the end: the last one again)
+        }
+        if (pop) break;
+        __syncthreads();
+#pragma unroll 1
+        for (int r = r0; r < r1; ++r) {
+            const int held = release && release[r] ? 0 : c.length[r];
+            push_at[r] = held;
+            c.length[r] = held + new_len[r];
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    deal_out(need_at, c.R, needed, [&](int r, int a, int b) { return stack[pushed - 1 - a]; },
-             [&](int r, int a, int b, int page) { entry(r, blocks_of(push_at[r]) + b) = page; });
     if (tid == 0) {
         cu[c.R] = tokens;
         c.n_free[0] = n_free + pushed - needed;
@@ -211,19 +205,31 @@ __device__ __forceinline__ int code_of(float x, int up, float amax1, float r) {
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }   // a NaN or an infinity is the largest
 
 // What the codes of a block with this amax are made with; codes are 0 in a block of zeros or with an infinity or a NaN.
+// 16-bit x (no shift): x (127 / amax) with 127 / amax in two parts, rounded once to fp32, is the exact quotient where that is a half
+// (k + 1/2 has 8 bits), and another quotient is at least 2^-20 of itself away from a half (127 X / A, X and A of 11 bits), so
+// it stays on its side: adding 1.5 2^23 + 128 rounds it as asked and leaves code + 128 in the low byte.  Shifted x has 24
+// bits and takes code_of, four times the instructions; so does an amax whose reciprocal leaves the normal range.
 struct Quantizer {
-    bool plain;
+    bool plain, fast;
     int up;
-    float amax1, inv;
+    float amax1, inv, hi, lo;
 
-    __device__ explicit Quantizer(uint32_t top) {
+    __device__ Quantizer(uint32_t top, bool shifted) {
         const float amax = __uint_as_float(top);
         plain = top > 0 && top < 0x7F800000u;
+        fast = !shifted && amax > 0x1p-60f && amax < 0x1p60f;
         up = plain ? 1 - __builtin_amdgcn_frexp_expf(amax) : 1;
         amax1 = plain ? __builtin_ldexpf(amax, up) : 1.0f, inv = 127.0f / amax1;
+        hi = __builtin_ldexpf(inv, up), lo = __builtin_ldexpf(__builtin_fmaf(-inv, amax1, 127.0f) * (inv * (1.0f / 127.0f)), up);
     }
-    __device__ __forceinline__ uint32_t byte(float x) const { return static_cast<uint32_t>((plain ? code_of(x, up, amax1, inv) : 0) + 128); }
+    // code + 128 in the low byte
+    __device__ __forceinline__ uint32_t quick(float x) const { return __float_as_uint(__builtin_fmaf(x, hi, x * lo) + 12583040.0f); }
+    __device__ __forceinline__ uint32_t slow(float x) const { return static_cast<uint32_t>((plain ? code_of(x, up, amax1, inv) : 0) + 128); }
 };
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    const uint32_t ab = __builtin_amdgcn_perm(b, a, 0x0c0c0400u), cd = __builtin_amdgcn_perm(d, c, 0x0c0c0400u);
+    return __builtin_amdgcn_perm(cd, ab, 0x05040100u);
+}
 
 // the largest of 256 threads' values; lds: 4
 __device__ __forceinline__ uint32_t workgroup_max(uint32_t v, uint32_t* lds) {
@@ -231,7 +237,7 @@ __device__ __forceinline__ uint32_t workgroup_max(uint32_t v, uint32_t* lds) {
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    return max(max(lds[0], lds[1]), max(lds[2], lds[3]));
+    return __builtin_amdgcn_readfirstlane(max(max(lds[0], lds[1]), max(lds[2], lds[3])));
 }
 
 // A workgroup quantizes one kv head's K or V of every page that begins to get tokens inside its window of `window` (a power of two
@@ -301,17 +307,17 @@ __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, co
             if (off == 0 || old >= now) {
                 done = true;
                 const uint32_t amax = max(old, now);
-                const Quantizer q(amax);
+                const Quantizer q(amax, shift != nullptr);
                 if (tok < n) {
                     uint32_t b[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) b[e] = q.byte(y[e]);
+                    for (int e = 0; e < 8; ++e) b[e] = q.fast ? q.quick(y[e]) : q.slow(y[e]);
                     if (is_v) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) codes[v_byte(off + tok, col + e)] = static_cast<uint8_t>(b[e]);
                     } else {
                         *reinterpret_cast<uint2*>(codes + k_byte(off + tok, col, D)) =
-                            make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+                            make_uint2(low_bytes(b[0], b[1], b[2], b[3]), low_bytes(b[4], b[5], b[6], b[7]));
                     }
                 }
                 if (tid == 0) (is_v ? c.v_amax : c.k_amax)[at] = __uint_as_float(amax);
@@ -355,28 +361,47 @@ __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, co
                 return shift && k_token(p) < off + n ? y - shift[k_channel(p) + e] : y;
             };
             uint32_t top = 0;
+            if (shift) {
 #pragma unroll
-            for (int p = 0; p < CV; ++p)
+                for (int p = 0; p < CV; ++p)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) top = max(top, abs_bits(value(p, e)));
+                    for (int e = 0; e < 16; ++e) top = max(top, abs_bits(value(p, e)));
+            } else {   // two 16-bit values at a time: their bits are ordered as their sizes
+                typedef unsigned short v2u __attribute__((ext_vector_type(2)));
+                v2u two = {0, 0};
+#pragma unroll
+                for (int p = 0; p < CV; ++p)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t bits = raw[p][e] & 0x7FFF7FFFu;
+                        v2u w;
+                        __builtin_memcpy(&w, &bits, 4);
+                        two = __builtin_elementwise_max(two, w);
+                    }
+                top = abs_bits(cvt16<DT>(max(two[0], two[1])));
+            }
             top = workgroup_max(top, lds_max);
-            const Quantizer q(top);
+            const Quantizer q(top, shift != nullptr);
 #pragma unroll
             for (int p = 0; p < CV; ++p)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(raw[p][e]));   // unpacked again, not kept as fp32 from the maximum on
+            auto write = [&](auto byte) {
 #pragma unroll
-            for (int p = 0; p < CV; ++p) {
-                uint32_t w[4];
+                for (int p = 0; p < CV; ++p) {
+                    uint32_t w[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    w[e] = q.byte(value(p, 4 * e)) | q.byte(value(p, 4 * e + 1)) << 8 | q.byte(value(p, 4 * e + 2)) << 16 | q.byte(value(p, 4 * e + 3)) << 24;
-                    __builtin_amdgcn_sched_barrier(0);
+                    for (int e = 0; e < 4; ++e) {
+                        w[e] = low_bytes(byte(value(p, 4 * e)), byte(value(p, 4 * e + 1)), byte(value(p, 4 * e + 2)), byte(value(p, 4 * e + 3)));
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    const int ch = CV * lane + p;
+                    const int piece = is_v ? (ch >> 4) * 64 + (ch & 15) + 16 * wave : (wave + 4 * p) * 64 + lane;
+                    reinterpret_cast<uint4*>(codes)[piece] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                const int ch = CV * lane + p;
-                const int piece = is_v ? (ch >> 4) * 64 + (ch & 15) + 16 * wave : (wave + 4 * p) * 64 + lane;
-                reinterpret_cast<uint4*>(codes)[piece] = make_uint4(w[0], w[1], w[2], w[3]);
-            }
+            };
+            if (q.fast) write([&](float y) { return q.quick(y); });
+            else write([&](float y) { return q.slow(y); });
             if (tid == 0) (is_v ? c.v_amax : c.k_amax)[at] = __uint_as_float(top);
         }
         if (i == row_begin) {   // the tokens of the row's last page, if it stays open (the older ones have been read: the maxima's barriers)
