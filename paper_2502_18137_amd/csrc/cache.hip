@@ -130,16 +130,16 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
     int32_t* stack = c.free_pages + n_free;
 #pragma unroll 1
     for (int pop = 0; pop < 2; ++pop) {
-        // page a of all that change hands is number a - prefix[r] of row r's; four a thread, one search, then along the rows,
+        // page a of all that change hands is number a - prefix[r] of row r's; eight a thread, one search, then along the rows,
         // all loads before the stores
         const int* prefix = pop ? need_at : push_at;
         const int n = pop ? needed : pushed;
 #pragma unroll 1
-        for (int a0 = 4 * tid; a0 < n; a0 += 4 * PLAN_THREADS) {
-            int r = row_of(prefix, c.R, a0), page[4];
-            int32_t* to[4];
+        for (int a0 = 8 * tid; a0 < n; a0 += 8 * PLAN_THREADS) {
+            int r = row_of(prefix, c.R, a0), page[8];
+            int32_t* to[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < 8; ++e) {
                 const int a = min(a0 + e, n - 1);
                 while (r + 1 < c.R && prefix[r + 1] <= a) ++r;
                 const int b = a - prefix[r] + (pop ? blocks_of(push_at[r]) : 0);
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
                 page[e] = *(pop ? place : entry);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) *to[e] = page[e];   // (beyond the end: the last one again)
+            for (int e = 0; e < 8; ++e) *to[e] = page[e];   // (beyond the end: the last one again)
         }
         if (pop) break;
         __syncthreads();
@@ -205,25 +205,32 @@ __device__ __forceinline__ int code_of(float x, int up, float amax1, float r) {
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }   // a NaN or an infinity is the largest
 
 // What the codes of a block with this amax are made with; codes are 0 in a block of zeros or with an infinity or a NaN.
-// 16-bit x (no shift): x (127 / amax) with 127 / amax in two parts, rounded once to fp32, is the exact quotient where that is a half
-// (k + 1/2 has 8 bits), and another quotient is at least 2^-20 of itself away from a half (127 X / A, X and A of 11 bits), so
-// it stays on its side: adding 1.5 2^23 + 128 rounds it as asked and leaves code + 128 in the low byte.  Shifted x has 24
-// bits and takes code_of, four times the instructions; so does an amax whose reciprocal leaves the normal range.
+// x (127 / amax) with 127 / amax in two parts, rounded once to fp32, is off by at most 2^-18.  For 16-bit x (no shift) that
+// decides every rounding: a quotient that is a half (k + 1/2 has 8 bits) comes out exact, and another is at least 2^-20 of
+// itself away from one (127 X / A, X and A of 11 bits), so it stays on its side: adding 1.5 2^23 + 128 rounds it as asked and
+// leaves code + 128 in the low byte.  Shifted x has 24 bits: where four quotients of a wave's lanes come near a half
+// (one time in a hundred) code_of decides, as it does where amax's reciprocal leaves the normal range.
 struct Quantizer {
     bool plain, fast;
     int up;
     float amax1, inv, hi, lo;
 
-    __device__ Quantizer(uint32_t top, bool shifted) {
+    __device__ explicit Quantizer(uint32_t top) {
         const float amax = __uint_as_float(top);
         plain = top > 0 && top < 0x7F800000u;
-        fast = !shifted && amax > 0x1p-60f && amax < 0x1p60f;
+        fast = amax > 0x1p-60f && amax < 0x1p60f;
         up = plain ? 1 - __builtin_amdgcn_frexp_expf(amax) : 1;
         amax1 = plain ? __builtin_ldexpf(amax, up) : 1.0f, inv = 127.0f / amax1;
         hi = __builtin_ldexpf(inv, up), lo = __builtin_ldexpf(__builtin_fmaf(-inv, amax1, 127.0f) * (inv * (1.0f / 127.0f)), up);
     }
     // code + 128 in the low byte
-    __device__ __forceinline__ uint32_t quick(float x) const { return __float_as_uint(__builtin_fmaf(x, hi, x * lo) + 12583040.0f); }
+    __device__ __forceinline__ uint32_t quick(float x) const { return __float_as_uint(__builtin_fmaf(x, hi, x * lo) + UP); }
+    // how near the quotient is to a half: the distance from its rounding
+    __device__ __forceinline__ float far(float x) const {
+        const float q = __builtin_fmaf(x, hi, x * lo);
+        return fabsf(q - ((q + UP) - UP));
+    }
+    static constexpr float UP = 12583040.0f, NEAR_HALF = 0.5f - 0x1p-16f;
     __device__ __forceinline__ uint32_t slow(float x) const { return static_cast<uint32_t>((plain ? code_of(x, up, amax1, inv) : 0) + 128); }
 };
 __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -307,11 +314,11 @@ __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, co
             if (off == 0 || old >= now) {
                 done = true;
                 const uint32_t amax = max(old, now);
-                const Quantizer q(amax, shift != nullptr);
+                const Quantizer q(amax);
                 if (tok < n) {
                     uint32_t b[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) b[e] = q.fast ? q.quick(y[e]) : q.slow(y[e]);
+                    for (int e = 0; e < 8; ++e) b[e] = q.fast && !shift ? q.quick(y[e]) : q.slow(y[e]);
                     if (is_v) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) codes[v_byte(off + tok, col + e)] = static_cast<uint8_t>(b[e]);
@@ -356,16 +363,19 @@ __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, co
                     __builtin_memcpy(raw[p], two, 32);
                 }
             }
-            auto value = [&](int p, int e) {
-                const float y = cvt16<DT>(static_cast<uint16_t>(raw[p][e >> 1] >> (16 * (e & 1))));
-                return shift && k_token(p) < off + n ? y - shift[k_channel(p) + e] : y;
-            };
+            float sh[16] = {};   // (the same channels for all p)
+            if (shift) {
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(sh + e) = *reinterpret_cast<const float4*>(shift + k_channel(0) + e);
+            }
+            auto plain_value = [&](int p, int e) { return cvt16<DT>(static_cast<uint16_t>(raw[p][e >> 1] >> (16 * (e & 1)))); };
+            auto shifted_value = [&](int p, int e) { return k_token(p) < off + n ? plain_value(p, e) - sh[e] : 0.f; };
             uint32_t top = 0;
             if (shift) {
 #pragma unroll
                 for (int p = 0; p < CV; ++p)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) top = max(top, abs_bits(value(p, e)));
+                    for (int e = 0; e < 16; ++e) top = max(top, abs_bits(shifted_value(p, e)));
             } else {   // two 16-bit values at a time: their bits are ordered as their sizes
                 typedef unsigned short v2u __attribute__((ext_vector_type(2)));
                 v2u two = {0, 0};
@@ -381,18 +391,18 @@ __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, co
                 top = abs_bits(cvt16<DT>(max(two[0], two[1])));
             }
             top = workgroup_max(top, lds_max);
-            const Quantizer q(top, shift != nullptr);
+            const Quantizer q(top);
 #pragma unroll
             for (int p = 0; p < CV; ++p)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(raw[p][e]));   // unpacked again, not kept as fp32 from the maximum on
-            auto write = [&](auto byte) {
+            auto write = [&](auto four) {
 #pragma unroll
                 for (int p = 0; p < CV; ++p) {
                     uint32_t w[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        w[e] = low_bytes(byte(value(p, 4 * e)), byte(value(p, 4 * e + 1)), byte(value(p, 4 * e + 2)), byte(value(p, 4 * e + 3)));
+                        w[e] = four(p, 4 * e);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                     const int ch = CV * lane + p;
@@ -400,8 +410,20 @@ __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, co
                     reinterpret_cast<uint4*>(codes)[piece] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             };
-            if (q.fast) write([&](float y) { return q.quick(y); });
-            else write([&](float y) { return q.slow(y); });
+            if (q.fast && !shift) {
+                write([&](int p, int e) {
+                    return low_bytes(q.quick(plain_value(p, e)), q.quick(plain_value(p, e + 1)), q.quick(plain_value(p, e + 2)), q.quick(plain_value(p, e + 3)));
+                });
+            } else {
+                write([&](int p, int e) {
+                    float y[4], far = 1.0f;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) y[k] = shift ? shifted_value(p, e + k) : plain_value(p, e + k);
+                    if (q.fast) far = fmaxf(fmaxf(q.far(y[0]), q.far(y[1])), fmaxf(q.far(y[2]), q.far(y[3])));
+                    if (__any(far > Quantizer::NEAR_HALF)) return low_bytes(q.slow(y[0]), q.slow(y[1]), q.slow(y[2]), q.slow(y[3]));
+                    return low_bytes(q.quick(y[0]), q.quick(y[1]), q.quick(y[2]), q.quick(y[3]));
+                });
+            }
             if (tid == 0) (is_v ? c.v_amax : c.k_amax)[at] = __uint_as_float(top);
         }
         if (i == row_begin) {   // the tokens of the row's last page, if it stays open (the older ones have been read: the maxima's barriers)

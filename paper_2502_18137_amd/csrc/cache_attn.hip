@@ -32,8 +32,9 @@ constexpr float P_UP_LOG2 = 8.0f;      // p is at most 2^4, its factor sv ratio 
                                        // weights down to 2^-33 of the largest are not lost
 constexpr float SV_LEAST = 0x1p-60f;   // smaller ratios (and blocks of zeros) count as this: below every rounding beside sv_ref
 
-constexpr int NARROW_ROWS = 16, NARROW_WGS = 512, NARROW_PARTS = 4 * NARROW_WGS;   // two workgroups per compute unit
-constexpr int WIDE_ROWS = 128, WIDE_WGS = 512;
+constexpr int NARROW_ROWS = 16, NARROW_WGS = 512, NARROW_LOG2 = 11;   // two workgroups per compute unit, a part per wave
+constexpr int WIDE_ROWS = 128, WIDE_WGS = 512, WIDE_LOG2 = 9;         // a part per workgroup
+static_assert(4 * NARROW_WGS == 1 << NARROW_LOG2 && WIDE_WGS == 1 << WIDE_LOG2, "the line is cut into up to 2^LOG2 parts");
 
 template <int X>
 __device__ __forceinline__ float other(float v) {   // of lane ^ X, X = 16 or 32
@@ -131,12 +132,32 @@ __device__ __forceinline__ u64 prefix(u64 v, u64* lds, u64& total) {
     return upto - v;
 }
 
+// a / b, both below 2^52.  (Kernels that run for a few microseconds wait for their own instructions: the 64-bit division that the
+// compiler would put in its place has 130 of them.)
+__device__ __forceinline__ u64 quotient(u64 a, u64 b) {
+    u64 q = static_cast<u64>(static_cast<double>(a) / static_cast<double>(b));
+    while (q * b > a) --q;
+    while ((q + 1) * b <= a) ++q;
+    return q;
+}
+
+// A line of `total` places in 2^log2 equal parts.
+struct Line {
+    u64 total;
+    int log2;
+
+    __device__ __forceinline__ u64 begin(int part) const { return (total * part) >> log2; }
+    __device__ __forceinline__ int part_of(u64 place) const {   // the last part that begins at or before a place
+        int p = static_cast<int>(static_cast<float>(place) / static_cast<float>(total) * static_cast<float>(1 << log2));
+        while (begin(p) > place) --p;
+        while (begin(p + 1) <= place) ++p;
+        return p;
+    }
+};
 // A part that begins inside an item: what the join needs.  start, end: the item on the line; token, head: its first.
-__device__ __forceinline__ JoinDesc boundary(u64 total, int parts, int part, u64 start, u64 end, int token, int n_tok, int head, int n_heads) {
-    int first = static_cast<int>(start * parts / total);                      // the first part that begins inside it
-    while (total * first / parts <= start) ++first;
-    const u64 last = (end * parts + total - 1) / total - 1;
-    return {static_cast<int>(last) - first + 2, first, part, token, n_tok, head, n_heads, 0};
+__device__ __forceinline__ JoinDesc boundary(const Line& line, int part, u64 start, u64 end, int token, int n_tok, int head, int n_heads) {
+    const int first = line.part_of(start) + 1;                   // the first part that begins inside it
+    return {line.part_of(end - 1) - first + 2, first, part, token, n_tok, head, n_heads, 0};
 }
 
 // The blocks of an item's range, 64 table entries at a time, one a lane, the next 64 on their way.
@@ -321,41 +342,44 @@ __device__ __forceinline__ void store_part(const v4f (&o)[NV], float m, float l,
 // Bound by the pages' bytes: a wave keeps the next block's K and V on their way while it works on one, 16 KB (d = 128), eight
 // waves on a compute unit; and it looks ahead over the end of an item, so that the next one's table, queries and first block
 // come while the last block of this one is worked on.
+struct NarrowShared {
+    u64 sums[4], rem[4];
+    int row[4];
+    RowInfo info[4];
+};
 template <int D, int DT>
-__global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache c, CacheAttn a, Rows which, const uint16_t* __restrict__ Q,
-                                                                   uint16_t* __restrict__ O, Joint ws) {
+__device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a, Rows which, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
+                                       const Joint& ws, int bid, NarrowShared& sh) {
     constexpr int NK = 4 * D / 64, NV = D / 16, KS = D / 32;
-    __shared__ u64 sums[4];
-    __shared__ u64 found_rem[4];
-    __shared__ int found_row[4];
-    __shared__ RowInfo found_info[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const Cut cut = cut_of(a.H / c.H_kv, NARROW_ROWS);
     const int heads = c.H_kv * cut.parts;
 
     // ---- this wave's part of the line, in blocks.  (All tiles of a row count with all its blocks: they are few here.)
     const int per = (c.R + 255) / 256;
-    auto length_of = [&](const RowInfo& x) { return static_cast<u64>(x.tiles) * heads * ((x.len + PAGE - 1) / PAGE); };
-    u64 mine = 0, total;
+    auto blocks_in = [&](const RowInfo& x) { return x.n ? (x.len + PAGE - 1) / PAGE : 0; };
+    auto length_of = [&](const RowInfo& x) { return static_cast<u64>(x.tiles) * heads * blocks_in(x); };
+    u64 mine = 0;
+    Line line;
+#pragma unroll 1
     for (int r = tid * per; r < min((tid + 1) * per, c.R); ++r) mine += length_of(row_info(c, a, cut, which, r));
-    const u64 before = prefix(mine, sums, total);
-    const int parts = static_cast<int>(min(total, static_cast<u64>(NARROW_PARTS)));
-    const int part = static_cast<int>(blockIdx.x) * 4 + wave;
+    const u64 before = prefix(mine, sh.sums, line.total);
+    line.total = uniform(line.total);
+    line.log2 = line.total >> NARROW_LOG2 ? NARROW_LOG2 : line.total ? 63 - __builtin_clzll(line.total) : 0;
+    const int parts = line.total ? 1 << line.log2 : 0, part = bid * 4 + wave;
+#pragma unroll 1
     for (int w = 0; w < 4; ++w) {
-        const int p = static_cast<int>(blockIdx.x) * 4 + w;
-        if (p >= parts) break;
-        const u64 at = total * p / parts;
-        if (before <= at && at < before + mine) {
+        const u64 at = line.begin(bid * 4 + w);
+        if (bid * 4 + w < parts && before <= at && at < before + mine) {
             u64 rem = at - before;
             int r = tid * per;
             RowInfo x = row_info(c, a, cut, which, r);
-            for (; rem >= length_of(x) && r < c.R - 1; x = row_info(c, a, cut, which, r)) {
+#pragma unroll 1
+            while (rem >= length_of(x) && r < c.R - 1) {
                 rem -= length_of(x);
-                ++r;
+                x = row_info(c, a, cut, which, ++r);
             }
-            found_row[w] = r;
-            found_rem[w] = rem;
-            found_info[w] = x;
+            sh.row[w] = r, sh.rem[w] = rem, sh.info[w] = x;
         }
     }
     __syncthreads();
@@ -363,49 +387,52 @@ __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache 
         if (lane == 0) ws.desc[part] = NO_JOIN;
         return;
     }
-    const u64 lo = uniform(total * part / parts);
-    u64 left = uniform(total * (part + 1) / parts) - lo;     // blocks that this wave still has to take
-    u64 rem = uniform(found_rem[wave]);                       // where in row `r` the next ones begin
-    int r = uniform(found_row[wave]);
+    // the next item's first block to take: row, of all heads' tiles the tile's number, block
+    int r = uniform(sh.row[wave]);
+    RowInfo info = uniform(sh.info[wave]);
+    int row_blocks = blocks_in(info);
+    const u64 lo = line.begin(part), rem = uniform(sh.rem[wave]);
+    u64 left = line.begin(part + 1) - lo;                     // blocks that this wave still has to take
+    const u64 in_row = row_blocks ? quotient(rem, row_blocks) : 0;
+    int b_next = static_cast<int>(rem - in_row * row_blocks);
+    int head = info.tiles ? static_cast<int>(quotient(in_row, info.tiles)) : 0;
+    int tile = static_cast<int>(in_row) - head * info.tiles;
     bool first_item = true;
-    RowInfo info = uniform(found_info[wave]);                 // row `r`
 
     struct Item {
         RowInfo x;
         int row, kh, gpart, tile, ntok, b0, b1, blocks;
     };
     auto next_item = [&](Item& it) -> bool {
-        while (left > 0 && r < c.R) {
-            it.x = info;
-            it.blocks = (it.x.len + PAGE - 1) / PAGE;
-            const u64 all = length_of(it.x);
-            if (rem >= all) {
-                rem -= all;
-                if (++r < c.R) info = uniform(row_info(c, a, cut, which, r));
-                continue;
+        if (left == 0) return false;
+        if (b_next == row_blocks) {     // on to the next tile, head, row
+            b_next = 0;
+            if (++tile >= info.tiles) tile = 0, ++head;
+            if (head >= heads) {
+                head = 0;
+                do {
+                    if (++r >= c.R) return false;
+                    info = uniform(row_info(c, a, cut, which, r));
+                    row_blocks = blocks_in(info);
+                } while (row_blocks == 0);
             }
-            const uint32_t tile = static_cast<uint32_t>(rem / static_cast<uint32_t>(it.blocks));   // of all heads' tiles
-            it.b0 = static_cast<int>(rem - static_cast<u64>(tile) * it.blocks);
-            const int head = static_cast<int>(tile / static_cast<uint32_t>(it.x.tiles));
-            it.tile = static_cast<int>(tile - static_cast<uint32_t>(head) * it.x.tiles);
-            it.row = r, it.kh = head / cut.parts, it.gpart = head - it.kh * cut.parts;
-            it.ntok = min(cut.TT, it.x.n - it.tile * cut.TT);
-            const u64 take = min(static_cast<u64>(it.blocks - it.b0), left);
-            it.b1 = it.b0 + static_cast<int>(take);
-            if (first_item) {
-                JoinDesc d = NO_JOIN;
-                const int g0 = it.gpart * NARROW_ROWS;
-                if (it.b0 > 0)
-                    d = boundary(total, parts, part, lo - it.b0, lo - it.b0 + it.blocks, it.x.first + it.tile * cut.TT, it.ntok,
-                                 it.kh * cut.G + g0, min(cut.Gp, cut.G - g0));
-                if (lane == 0) ws.desc[part] = d;
-                first_item = false;
-            }
-            left -= take;
-            rem += take;
-            return true;
         }
-        return false;
+        it.x = info, it.row = r, it.tile = tile, it.blocks = row_blocks, it.b0 = b_next;
+        it.kh = head / cut.parts, it.gpart = head - it.kh * cut.parts;
+        it.ntok = min(cut.TT, info.n - tile * cut.TT);
+        const int take = static_cast<int>(min(static_cast<u64>(row_blocks - b_next), left));
+        it.b1 = b_next += take;
+        left -= take;
+        if (first_item) {
+            first_item = false;
+            JoinDesc d = NO_JOIN;
+            const int g0 = it.gpart * NARROW_ROWS;
+            if (it.b0 > 0)
+                d = boundary(line, part, lo - it.b0, lo - it.b0 + it.blocks, info.first + tile * cut.TT, it.ntok, it.kh * cut.G + g0,
+                             min(cut.Gp, cut.G - g0));
+            if (lane == 0) ws.desc[part] = d;
+        }
+        return true;
     };
 
     Blocks blocks;
@@ -558,14 +585,19 @@ __device__ __forceinline__ float convert_q32(const uint4 (&raw)[D / 16], v8h (&q
 // (two buffers, one barrier a block; the raw bytes of the block after the next are on their way meanwhile), and every wave
 // reads them for its own 32 query rows.  In that MFMA's accumulators a lane owns one query (lane % 32) and, of every 16 keys,
 // 4 (lane / 32) + 0..3 and those + 8; V's operands are laid out for that order.
+template <int D>
+struct WideShared {
+    u64 sums[4], rem;
+    int row;
+    RowInfo info;
+    __align__(16) v8h k[2][2 * D / 16 * 64], v[2][D / 32 * 4 * 64];
+};
 template <int D, int DT>
-__global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c, CacheAttn a, Rows which, const uint16_t* __restrict__ Q,
-                                                                 uint16_t* __restrict__ O, Joint ws) {
+__device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, Rows which, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
+                                     const Joint& ws, int bid, WideShared<D>& sh) {
     constexpr int KS = D / 16, NC = D / 32, RAW = D / 64;   // steps of K Q^T, channel tiles, 16-byte pieces of K (of V) per thread
-    __shared__ u64 sums[4];
-    __shared__ u64 found_rem;
-    __shared__ int found_row;
-    __shared__ __align__(16) v8h lds_k[2][2 * KS * 64], lds_v[2][NC * 4 * 64];
+    auto& lds_k = sh.k;
+    auto& lds_v = sh.v;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
     const Cut cut = cut_of(a.H / c.H_kv, WIDE_ROWS);
     const int heads = c.H_kv * cut.parts;
@@ -573,58 +605,57 @@ __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c,
     // ---- this workgroup's part of the line, in keys
     const int per = (c.R + 255) / 256;
     auto length_of = [&](const RowInfo& x) { return sum_vis(x, cut, a.causal, x.tiles); };
-    u64 mine = 0, total;
+    u64 mine = 0;
+    Line line;
+#pragma unroll 1
     for (int r = tid * per; r < min((tid + 1) * per, c.R); ++r) mine += length_of(row_info(c, a, cut, which, r)) * heads;
-    const u64 before = prefix(mine, sums, total);
-    // equal parts of at least two blocks; a multiple of 8, so that neighbours on the line, which share pages, are neighbours on an XCD
-    const u64 wanted = total / (2 * PAGE);
-    const int parts = wanted >= WIDE_WGS ? WIDE_WGS : wanted >= 8 ? static_cast<int>(wanted) & ~7 : wanted >= 1 ? static_cast<int>(wanted) : total > 0;
-    const int bid = blockIdx.x;
+    const u64 before = prefix(mine, sh.sums, line.total);
+    line.total = uniform(line.total);
+    // parts of at least two blocks; neighbours on the line, which share pages, are neighbours on an XCD
+    const u64 wanted = line.total / (2 * PAGE);
+    line.log2 = wanted >> WIDE_LOG2 ? WIDE_LOG2 : wanted ? 63 - __builtin_clzll(wanted) : 0;
+    const int parts = line.total ? 1 << line.log2 : 0;
     if (bid >= parts) {
         if (tid == 0) ws.desc[bid] = NO_JOIN;
         return;
     }
-    const int part = parts >= 8 ? (bid & 7) * (parts / 8) + (bid >> 3) : bid;
-    const u64 lo = uniform(total * part / parts), hi = uniform(total * (part + 1) / parts);
+    const int part = parts >= 8 ? (bid & 7) * (parts >> 3) + (bid >> 3) : bid;
+    const u64 lo = line.begin(part);
     if (before <= lo && lo < before + mine) {
         u64 rem = lo - before;
         int r = tid * per;
-        for (; r < c.R - 1; ++r) {
-            const u64 all = length_of(row_info(c, a, cut, which, r)) * heads;
-            if (rem < all) break;
-            rem -= all;
+        RowInfo x = row_info(c, a, cut, which, r);
+#pragma unroll 1
+        while (rem >= length_of(x) * heads && r < c.R - 1) {
+            rem -= length_of(x) * heads;
+            x = row_info(c, a, cut, which, ++r);
         }
-        found_row = r;
-        found_rem = rem;
+        sh.row = r, sh.rem = rem, sh.info = x;
     }
     __syncthreads();
-    int r = uniform(found_row);
-    u64 rem = uniform(found_rem), pos = lo;
+    int r = uniform(sh.row);
+    RowInfo x = uniform(sh.info);
+    u64 left = line.begin(part + 1) - lo;                     // keys that this workgroup still has to take
     JoinDesc join = NO_JOIN;
+    // where it begins: head (with the group's part), tile, key
+    const u64 rem = uniform(sh.rem), chunk = max(length_of(x), static_cast<u64>(1));
+    int head = static_cast<int>(quotient(rem, chunk)), i = 0;
+    const u64 in = rem - head * chunk;
+#pragma unroll 1
+    for (int up = x.tiles; up - i > 1;) {
+        const int mid = (i + up) >> 1;
+        if (sum_vis(x, cut, a.causal, mid) <= in) i = mid; else up = mid;
+    }
+    int x0 = static_cast<int>(in - sum_vis(x, cut, a.causal, i));
 
-    while (pos < hi && r < c.R) {
-        const RowInfo x = uniform(row_info(c, a, cut, which, r));
-        const u64 chunk = length_of(x);
-        if (rem >= chunk * heads) {
-            rem -= chunk * heads;
-            ++r;
-            continue;
-        }
-        const int head = static_cast<int>(rem / chunk);   // kv head and part of its group
-        const u64 in = rem - head * chunk;
-        int i = 0;
-        for (int up = x.tiles; up - i > 1;) {
-            const int mid = (i + up) >> 1;
-            if (sum_vis(x, cut, a.causal, mid) <= in) i = mid; else up = mid;
-        }
-        const int x0 = static_cast<int>(in - sum_vis(x, cut, a.causal, i));
+    while (left > 0) {
         const int ntok = min(cut.TT, x.n - i * cut.TT), token0 = x.first + i * cut.TT;
         const int kh = head / cut.parts, g0 = (head - kh * cut.parts) * WIDE_ROWS, n_heads = min(cut.Gp, cut.G - g0);
         const int vis = a.causal ? x.p0 + i * cut.TT + ntok : x.len;
-        const int take = static_cast<int>(min(static_cast<u64>(vis - x0), hi - pos)), x1 = x0 + take;
+        const int take = static_cast<int>(min(static_cast<u64>(vis - x0), left)), x1 = x0 + take;
         const int b0 = x0 / PAGE, b1 = x1 == vis ? (vis + PAGE - 1) / PAGE : x1 / PAGE;
-        const bool whole = x0 == 0 && x1 == vis;
-        if (pos == lo && x0 > 0) join = boundary(total, parts, part, lo - x0, lo - x0 + vis, token0, ntok, kh * cut.G + g0, n_heads);
+        const bool whole = x0 == 0 && x1 == vis, is_first = left == line.begin(part + 1) - lo;
+        if (is_first && x0 > 0) join = boundary(line, part, lo - x0, lo - x0 + vis, token0, ntok, kh * cut.G + g0, n_heads);
 
         // this wave's rows, the lane's one of them, and the least and the largest key that a row sees last
         const int n_rows = ntok * cut.Gp, w0 = wave * 32, w1 = min(w0 + 32, n_rows) - 1;
@@ -803,10 +834,42 @@ __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c,
                 }
             if (!whole && half == 0) ws.ml[2 * row_at] = m, ws.ml[2 * row_at + 1] = l;
         }
-        pos += take;
-        rem += take;
+        // on to the next tile, head, row
+        left -= take;
+        x0 = 0;
+        if (++i >= x.tiles) i = 0, ++head;
+        if (head >= heads && left > 0) {
+            head = 0;
+            do {
+                if (++r >= c.R) left = 0;     // (cannot be: the line ends with the rows)
+                else x = uniform(row_info(c, a, cut, which, r));
+            } while (left > 0 && x.n == 0);
+        }
     }
     if (tid == 0) ws.desc[bid] = join;
+}
+
+// ---- the launches: rows of the one kind, of the other, or both side by side
+template <int D, int DT>
+__global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache c, CacheAttn a, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O, Joint ws) {
+    __shared__ NarrowShared sh;
+    narrow<D, DT>(c, a, ALL_ROWS, Q, O, ws, blockIdx.x, sh);
+}
+template <int D, int DT>
+__global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c, CacheAttn a, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O, Joint ws) {
+    __shared__ WideShared<D> sh;
+    wide<D, DT>(c, a, ALL_ROWS, Q, O, ws, blockIdx.x, sh);
+}
+template <int D, int DT>
+__global__ __launch_bounds__(256, 2) void cache_attn_both_kernel(sparge_cache c, CacheAttn a, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
+                                                                 Joint ws_wide, Joint ws_narrow) {
+    __shared__ union Shared {
+        __device__ Shared() {}
+        WideShared<D> wide;
+        NarrowShared narrow;
+    } sh;
+    if (blockIdx.x < WIDE_WGS) wide<D, DT>(c, a, MANY_ROWS, Q, O, ws_wide, blockIdx.x, sh.wide);
+    else narrow<D, DT>(c, a, FEW_ROWS, Q, O, ws_narrow, blockIdx.x - WIDE_WGS, sh.narrow);
 }
 
 // ---- join ----------------------------------------------------------------------------------------------------------
@@ -871,45 +934,50 @@ __device__ __forceinline__ void join_item(const JoinDesc& d, int me, int workers
 }
 // WAVES: of a workgroup, for one description
 template <int D, int DT, int ROWS, int WAVES>
-__global__ __launch_bounds__(256) void cache_join_kernel(sparge_cache c, CacheAttn a, uint16_t* __restrict__ O, Joint ws) {
+__device__ __forceinline__ void join(const sparge_cache& c, const CacheAttn& a, uint16_t* O, const Joint& ws, int bid) {
     const int wave = uniform(static_cast<int>(threadIdx.x) >> 6);
-    const JoinDesc d = ws.desc[(blockIdx.x * 4 + wave) / WAVES];
+    const JoinDesc d = ws.desc[(bid * 4 + wave) / WAVES];
     if (d.n_parts == 0) return;
     const int Gp = cut_of(a.H / c.H_kv, ROWS).Gp, me = (d.part - d.first) * WAVES + wave % WAVES, workers = (d.n_parts - 1) * WAVES;
     if (d.n_parts <= 4) join_item<D, DT, ROWS, 1>(d, me, workers, Gp, a, O, ws);
     else join_item<D, DT, ROWS, 8>(d, me, workers, Gp, a, O, ws);
 }
+// the first n_wide workgroups take the wide kernel's parts, the others the narrow one's
+template <int D, int DT>
+__global__ __launch_bounds__(256) void cache_join_kernel(sparge_cache c, CacheAttn a, int n_wide, uint16_t* __restrict__ O, Joint ws_wide, Joint ws_narrow) {
+    const int bid = blockIdx.x;
+    if (bid < n_wide) join<D, DT, WIDE_ROWS, 4>(c, a, O, ws_wide, bid);
+    else join<D, DT, NARROW_ROWS, 1>(c, a, O, ws_narrow, bid - n_wide);
+}
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
-// The workspace: descriptions, references and sums, partial rows.  The two kernels use the same room one after the other.
-constexpr size_t MOST_ROWS = 2ull * (NARROW_PARTS * NARROW_ROWS > WIDE_WGS * WIDE_ROWS ? NARROW_PARTS * NARROW_ROWS : WIDE_WGS * WIDE_ROWS);
+// The workspace, once per kernel: descriptions, references and sums, partial rows.
 struct Layout {
-    size_t ml, o, total;
+    size_t desc[2], ml[2], o[2], total;   // wide, narrow
 };
 Layout layout_of(int d) {
-    const size_t up = 255;
+    const size_t parts[2] = {1u << WIDE_LOG2, 1u << NARROW_LOG2}, rows[2] = {2 * parts[0] * WIDE_ROWS, 2 * parts[1] * NARROW_ROWS};
     Layout x;
-    x.ml = (NARROW_PARTS * sizeof(JoinDesc) + up) & ~up;
-    x.o = x.ml + MOST_ROWS * 2 * sizeof(float);
-    x.total = x.o + MOST_ROWS * d * sizeof(float);
+    size_t at = 0;
+    for (int k = 0; k < 2; ++k) {
+        x.desc[k] = at, at += parts[k] * sizeof(JoinDesc);
+        x.ml[k] = at, at += rows[k] * 2 * sizeof(float);
+        x.o[k] = at, at += rows[k] * d * sizeof(float);
+    }
+    x.total = at;
     return x;
 }
 
 template <int D, int DT>
-void launch(const sparge_cache& c, const CacheAttn& a, bool narrow, bool wide, const void* Qp, void* Op, const Joint& j, hipStream_t st) {
+void launch(const sparge_cache& c, const CacheAttn& a, bool narrow, bool wide, const void* Qp, void* Op, const Joint (&j)[2], hipStream_t st) {
     const uint16_t* Q = static_cast<const uint16_t*>(Qp);
     uint16_t* O = static_cast<uint16_t*>(Op);
-    if (narrow) {
-        const Rows which = wide ? FEW_ROWS : ALL_ROWS;
-        hipLaunchKernelGGL((cache_attn_narrow_kernel<D, DT>), dim3(NARROW_WGS), dim3(256), 0, st, c, a, which, Q, O, j);
-        hipLaunchKernelGGL((cache_join_kernel<D, DT, NARROW_ROWS, 1>), dim3(NARROW_PARTS / 4), dim3(256), 0, st, c, a, O, j);
-    }
-    if (wide) {
-        const Rows which = narrow ? MANY_ROWS : ALL_ROWS;
-        hipLaunchKernelGGL((cache_attn_wide_kernel<D, DT>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, which, Q, O, j);
-        hipLaunchKernelGGL((cache_join_kernel<D, DT, WIDE_ROWS, 4>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, O, j);
-    }
+    if (narrow && wide) hipLaunchKernelGGL((cache_attn_both_kernel<D, DT>), dim3(WIDE_WGS + NARROW_WGS), dim3(256), 0, st, c, a, Q, O, j[0], j[1]);
+    else if (wide) hipLaunchKernelGGL((cache_attn_wide_kernel<D, DT>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, Q, O, j[0]);
+    else hipLaunchKernelGGL((cache_attn_narrow_kernel<D, DT>), dim3(NARROW_WGS), dim3(256), 0, st, c, a, Q, O, j[1]);
+    const int n_wide = wide ? WIDE_WGS : 0, n_narrow = narrow ? NARROW_WGS : 0;
+    hipLaunchKernelGGL((cache_join_kernel<D, DT>), dim3(n_wide + n_narrow), dim3(256), 0, st, c, a, n_wide, O, j[0], j[1]);
 }
 
 }  // namespace
@@ -919,13 +987,16 @@ size_t cache_attn_workspace(int d) { return layout_of(d).total; }
 hipError_t launch_cache_attn(const sparge_cache& c, const CacheAttn& a, const void* Q, void* O, void* ws, hipStream_t st) {
     const Layout x = layout_of(c.d);
     char* p = static_cast<char*>(ws);
-    const Joint j = {reinterpret_cast<JoinDesc*>(p), reinterpret_cast<float*>(p + x.ml), reinterpret_cast<float*>(p + x.o)};
-    // How many tokens each row adds is not known here.  With no more tokens than rows, one each is the case to be fast in, whose
-    // group fits a wave or does not; with a single row it is known; else both kernels run, each on its rows.
-    const int G = a.H / c.H_kv;
-    const bool one_kind = a.n_slots <= c.R || c.R == 1;
-    const bool few = static_cast<long long>(c.R == 1 ? a.n_slots : 1) * G <= NARROW_ROWS;
-    const bool narrow = one_kind ? few : G <= NARROW_ROWS, wide = one_kind ? !few : true;
+    Joint j[2];
+    for (int k = 0; k < 2; ++k)
+        j[k] = {reinterpret_cast<JoinDesc*>(p + x.desc[k]), reinterpret_cast<float*>(p + x.ml[k]), reinterpret_cast<float*>(p + x.o[k])};
+    // How many tokens each row adds is not known here.  Groups beyond a wave's 16 rows are the wide kernel's.  Up to 16 tokens
+    // more than rows (one each, and what pads a batch), or up to half a wave's rows on average, are taken for decoding: the
+    // narrow kernel alone, which gives the right result for longer rows, too.  A single row of more is the wide kernel's; else both
+    // run side by side, each on its rows.
+    const long long G = a.H / c.H_kv;
+    const bool few = a.n_slots <= c.R + 16 || a.n_slots * G <= NARROW_ROWS / 2 * c.R;
+    const bool narrow = G <= NARROW_ROWS && (few || c.R > 1), wide = G > NARROW_ROWS || !few;
 #define RUN(D, DT) launch<D, DT>(c, a, narrow, wide, Q, O, j, st)
     if (c.d == 64) {
         if (c.dtype == SPARGE_F16) RUN(64, SPARGE_F16); else RUN(64, SPARGE_BF16);

@@ -155,7 +155,7 @@ def test_workspace_size(lib):
     for d in (64, 128):
         assert lib.sparge_cache_attn_workspace_bytes(cache(d=d), 4, ctypes.byref(n)) == 0
         refused(attn(lib, cache(d=d), s=(1024, 128), o=(1024, 128), size=n.value - 1), -3, lib)
-        assert n.value <= 80 << 20
+        assert n.value <= 100 << 20
     refused(lib.sparge_cache_attn_workspace_bytes(cache(), 5, ctypes.byref(n)), -1, lib)
     refused(lib.sparge_cache_attn_workspace_bytes(cache(), 130, ctypes.byref(n)), -2, lib)
 
