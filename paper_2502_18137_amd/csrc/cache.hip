@@ -130,26 +130,50 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
     int32_t* stack = c.free_pages + n_free;
 #pragma unroll 1
     for (int pop = 0; pop < 2; ++pop) {
-        // page a of all that change hands is number a - prefix[r] of row r's; eight a thread, one search, then along the rows,
-        // all loads before the stores
+        // Groups of 64 rows are dealt out over the waves (a group to several where there are few), a lane counts a row's pages in
+        // pieces of 64, and the wave takes the pieces one after the other, eight at a time on their way.  (Pages dealt out over
+        // the threads, each looking up its row, take 17 to 25 us where this takes PLAN_US: one compute unit's issue.)
         const int* prefix = pop ? need_at : push_at;
-        const int n = pop ? needed : pushed;
+        const int n = pop ? needed : pushed, groups = (c.R + 63) / 64, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        constexpr int WAVES = PLAN_THREADS / 64;
+        const int log2 = groups > 1 ? min(4, 32 - __builtin_clz(groups - 1)) : 0, sharers = WAVES >> log2, share = wave >> log2;
 #pragma unroll 1
-        for (int a0 = 8 * tid; a0 < n; a0 += 8 * PLAN_THREADS) {
-            int r = row_of(prefix, c.R, a0), page[8];
-            int32_t* to[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int a = min(a0 + e, n - 1);
-                while (r + 1 < c.R && prefix[r + 1] <= a) ++r;
-                const int b = a - prefix[r] + (pop ? blocks_of(push_at[r]) : 0);
-                int32_t* entry = c.table + static_cast<long long>(r) * c.max_blocks + b;
-                int32_t* place = stack + (pop ? pushed - 1 - a : a);
-                to[e] = pop ? entry : place;
-                page[e] = *(pop ? place : entry);
+        for (int g = wave & ((1 << log2) - 1); g < groups; g += 1 << log2) {
+            const int r = 64 * g + lane;
+            int count = 0, base = 0, first = 0;
+            if (r < c.R) {
+                base = prefix[r], count = (r + 1 < c.R ? prefix[r + 1] : n) - base;
+                if (pop) first = blocks_of(push_at[r]);
             }
+            const int pieces = (count + 63) / 64;
+            int upto = pieces;
+#pragma unroll 1
+            for (int s = 1; s < 64; s <<= 1) {
+                const int y = __shfl_up(upto, s);
+                if (lane >= s) upto += y;
+            }
+            const int all = __builtin_amdgcn_readlane(upto, 63);
+#pragma unroll 1
+            for (int k0 = 8 * share; k0 < all; k0 += 8 * sharers) {
+                int page[8];
+                int32_t* to[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) *to[e] = page[e];   // (beyond the end: the last one again)
+                for (int e = 0; e < 8; ++e) {
+                    to[e] = nullptr;
+                    if (k0 + e >= all) continue;
+                    const int at = __builtin_popcountll(__ballot(upto <= k0 + e));   // the row's lane
+                    const int b = 64 * (k0 + e - __builtin_amdgcn_readlane(upto - pieces, at)) + lane;
+                    if (b >= __builtin_amdgcn_readlane(count, at)) continue;
+                    const int a = __builtin_amdgcn_readlane(base, at) + b;
+                    int32_t* entry = c.table + static_cast<long long>(64 * g + at) * c.max_blocks + __builtin_amdgcn_readlane(first, at) + b;
+                    int32_t* place = stack + (pop ? pushed - 1 - a : a);
+                    to[e] = pop ? entry : place;
+                    page[e] = *(pop ? place : entry);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (to[e]) *to[e] = page[e];
+            }
         }
         if (pop) break;
         __syncthreads();

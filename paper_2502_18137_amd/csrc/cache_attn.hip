@@ -26,9 +26,9 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef unsigned long long u64;
 
 constexpr float FAR = -1e30f;          // reference of a row that has seen no key
-constexpr float SLACK = 4.0f;          // log2: how far a row's maximum may run ahead of the reference inside exp2
-constexpr float SV_SLACK = 4.0f;       // how far a block's V scale may exceed the one that O is relative to
-constexpr float P_UP_LOG2 = 8.0f;      // p is at most 2^4, its factor sv ratio at most 4: p x ratio x 2^8 <= 2^14 in fp16, and
+constexpr float SLACK = 6.0f;          // log2: how far a row's maximum may run ahead of the reference inside exp2
+constexpr float SV_SLACK = 2.0f;       // how far a block's V scale may exceed the one that O is relative to
+constexpr float P_UP_LOG2 = 8.0f;      // p is at most 2^6, its factor sv ratio at most 2: p x ratio x 2^8 <= 2^15 in fp16, and
                                        // weights down to 2^-33 of the largest are not lost
 constexpr float SV_LEAST = 0x1p-60f;   // smaller ratios (and blocks of zeros) count as this: below every rounding beside sv_ref
 
@@ -266,8 +266,8 @@ struct VScale {
     // -> what O has to be multiplied with first (1: nothing)
     __device__ __forceinline__ float take(float va) {
         float down = 1.0f;
-        if (va > SV_SLACK * ref) down = ref / va, ref = va;
-        float f = va / ref;
+        if (va > SV_SLACK * ref) down = ref * __builtin_amdgcn_rcpf(va), ref = va;
+        float f = va * __builtin_amdgcn_rcpf(ref);
         if (va < SV_LEAST * ref || va == 0.f) f = SV_LEAST;   // (a block of zeros has codes 0 whatever the factor)
         f_log2 = __builtin_amdgcn_logf(f) + P_UP_LOG2, f_inv = __builtin_amdgcn_rcpf(f) * 0x1p-8f;
         return down;
@@ -552,6 +552,11 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
     }
 }
 
+// A barrier for what goes through LDS: loads from memory that are on their way stay on it (__syncthreads waits for them).
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 // ---- many query rows: four waves share the blocks --------------------------------------------------------------------
 
 __device__ __forceinline__ u64 sum_vis(const RowInfo& x, const Cut& t, bool causal, int i) {   // keys that the tiles before i see
@@ -675,7 +680,7 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
             if (valid) q_raw[s] = *reinterpret_cast<const uint4*>(Q + token * a.q_sn + hd * a.q_sh + 16 * s + 8 * half);
         }
 
-        uint4 kraw[RAW], vraw[RAW];
+        uint4 kraw[RAW] = {}, vraw[RAW] = {};
         auto load_raw = [&](int page) {
             const long long at = (static_cast<long long>(page) * c.H_kv + kh) * (PAGE * D) + tid * 16;
 #pragma unroll
@@ -684,27 +689,28 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
                 vraw[n] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(c.v) + at + n * 4096);
             }
         };
-        auto convert = [&](int buf) {
-            const int l16 = lane & 15, gr = lane >> 4;
-#pragma unroll
-            for (int n = 0; n < RAW; ++n) {
-                const int piece = wave + 4 * n;
+        // a quarter of a thread's pieces n (K's first and second half, V's first and second) into LDS
+        constexpr int CHUNKS = 4 * RAW;
+        auto convert_chunk = [&](int buf, int chunk) {
+            const int l16 = lane & 15, gr = lane >> 4, n = chunk >> 2, which = chunk & 3, piece = wave + 4 * n;
+            if (which < 2) {
                 // K: keys 16 t + l16, channels 64 e + 16 gr + 0..15: step 4 e + gr of key tile t / 2, eight channels a half
                 const int t = piece / (D / 64), e = piece - t * (D / 64);
-                v8h* k = &lds_k[buf][((t >> 1) * KS + 4 * e + gr) * 64 + 16 * (t & 1) + l16];
-                k[0] = codes8(kraw[n].x, kraw[n].y);
-                k[32] = codes8(kraw[n].z, kraw[n].w);
+                lds_k[buf][((t >> 1) * KS + 4 * e + gr) * 64 + 16 * (t & 1) + l16 + 32 * which] =
+                    which ? codes8(kraw[n].z, kraw[n].w) : codes8(kraw[n].x, kraw[n].y);
+            } else {
                 // V: channel 16 piece + l16, keys 16 t + 4 gr + 0..3 in word t: step t, half gr % 2, place 4 (gr / 2)
                 uint2* v = reinterpret_cast<uint2*>(&lds_v[buf][(piece >> 1) * 4 * 64 + 16 * (piece & 1) + l16 + 32 * (gr & 1)]) + (gr >> 1);
-                const v8h v01 = codes8(vraw[n].x, vraw[n].y), v23 = codes8(vraw[n].z, vraw[n].w);
-                uint4 w01, w23;
-                __builtin_memcpy(&w01, &v01, 16);
-                __builtin_memcpy(&w23, &v23, 16);
-                v[0] = make_uint2(w01.x, w01.y);
-                v[128] = make_uint2(w01.z, w01.w);
-                v[256] = make_uint2(w23.x, w23.y);
-                v[384] = make_uint2(w23.z, w23.w);
+                const v8h two = which == 2 ? codes8(vraw[n].x, vraw[n].y) : codes8(vraw[n].z, vraw[n].w);
+                uint4 w;
+                __builtin_memcpy(&w, &two, 16);
+                v[256 * (which - 2)] = make_uint2(w.x, w.y);
+                v[256 * (which - 2) + 128] = make_uint2(w.z, w.w);
             }
+        };
+        auto convert = [&](int buf) {
+#pragma unroll
+            for (int x = 0; x < CHUNKS; ++x) convert_chunk(buf, x);
         };
         int block = 0, page = 0, at = 0, n_block = 0, n_at = 0;
         float ka = 0.f, va = 0.f, n_ka = 0.f, n_va = 0.f;
@@ -731,15 +737,30 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
             }
         }
         __syncthreads();
-        auto step = [&](bool masked, int buf) {
-            v16f s[2];
+        // Scores of a block beside the conversion of the next one, and, in weigh, O beside the weights.  The order is laid down
+        // (nothing crosses the sched_barriers): operands are read four products ahead; left to itself the compiler reads
+        // one, waits for it and issues its product.
+        v16f s[2];
+        auto scores = [&](int buf) {
+            v8h k[4];
+            auto operand = [&](int x) { return lds_k[buf][((x & 1) * KS + (x >> 1)) * 64 + lane]; };
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int x = 0; x < 4; ++x) k[x] = operand(x);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int e = 0; e < KS; ++e) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_k[buf][(t * KS + e) * 64 + lane], qf[e], s[t], 0, 0, 0);
+            for (int x = 0; x < 2 * KS; ++x) {
+                s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[x & 3], qf[x >> 1], s[x & 1], 0, 0, 0);
+                if (x + 4 < 2 * KS) k[x & 3] = operand(x + 4);
+                if (x & 1) convert_chunk(buf ^ 1, x >> 1);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            static_assert(CHUNKS == KS, "a chunk for every other product");
+        };
+        auto weigh = [&](bool masked, int buf) {
             float cq = qs * ka;
             if (cq == 0.f) cq = 1e-37f;   // a block of zeros: -inf stays what it is and becomes a weight of 0
             const int last = limit - block * PAGE - 4 * half;   // key 32 t + 8 (e / 4) + e % 4 of the lane's
@@ -769,41 +790,62 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
             }
             const float from = vs.f_log2 - m;
             float sum = 0.f;
-            v8h pf[4];
+            v8h pf[4], v[4];
+            auto weights = [&](int u, int e) {   // two of the eight of step u
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                float w[8];
+                for (int k = e; k < e + 2; ++k) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + k], cq, from));
+                    sum += w;
+                    pf[u][k] = static_cast<_Float16>(w);
+                }
+                asm volatile("" : "+v"(sum));   // here, not all of them behind the last product
+            };
+            auto operand = [&](int x) { return lds_v[buf][((x % NC) * 4 + x / NC) * 64 + lane]; };
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + e], cq, from));
+            for (int x = 0; x < 4; ++x) v[x] = operand(x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += w[e];
+            for (int e = 0; e < 8; e += 2) weights(0, e);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) pf[u][e] = static_cast<_Float16>(w[e]);
+            for (int x = 0; x < 4 * NC; ++x) {
+                const int u = x / NC, n = x % NC;
+                o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x & 3], pf[u], o[n], 0, 0, 0);
+                if (x + 4 < 4 * NC) v[x & 3] = operand(x + 4);
+                if (u < 3) {
 #pragma unroll
-                for (int n = 0; n < NC; ++n) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_v[buf][(n * 4 + u) * 64 + lane], pf[u], o[n], 0, 0, 0);
+                    for (int e = 8 / NC * n; e < 8 / NC * (n + 1); e += 2) weights(u + 1, e);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
             l += sum * vs.f_inv;
         };
         for (int buf = 0; more; buf ^= 1) {
-            // the next block's bytes into the other buffer, the one after it on its way
+            // the next block's bytes into the other buffer (nobody reads it; behind the last block whatever is there), the one
+            // after it on its way
+            const bool mine = block * PAGE <= lim_hi;
+            if (mine) {
+                scores(buf);
+            } else {
+#pragma unroll
+                for (int n = 0; n < RAW; ++n)   // (that the two conversions have nothing to be drawn together from)
+                    asm volatile("" : "+v"(kraw[n].x), "+v"(kraw[n].y), "+v"(kraw[n].z), "+v"(kraw[n].w), "+v"(vraw[n].x), "+v"(vraw[n].y),
+                                 "+v"(vraw[n].z), "+v"(vraw[n].w));
+                convert(buf ^ 1);
+            }
             int nn_block = 0, nn_at = 0;
             float nn_ka = 0.f, nn_va = 0.f;
-            bool nn_more = false;
-            if (n_more) {
-                convert(buf ^ 1);
-                nn_more = blocks.next(c, kh, nn_block, page, nn_at);
-                if (nn_more) {
-                    load_raw(page);
-                    nn_ka = blocks.ka(nn_at), nn_va = blocks.va(nn_at);
-                }
+            const bool nn_more = n_more && blocks.next(c, kh, nn_block, page, nn_at);
+            if (nn_more) {
+                load_raw(page);
+                nn_ka = blocks.ka(nn_at), nn_va = blocks.va(nn_at);
             }
-            if (block * PAGE <= lim_hi) {
+            if (mine) {
                 const bool bad = not_finite(ka, va);
                 if (bad) ka = va = 0.f;
-                step(block * PAGE + PAGE - 1 > lim_lo, buf);
+                weigh(block * PAGE + PAGE - 1 > lim_lo, buf);
                 if (bad && limit >= block * PAGE) l = nan_f();
             }
-            __syncthreads();
+            lds_barrier();
             more = n_more, block = n_block, ka = n_ka, va = n_va;
             n_more = nn_more, n_block = nn_block, n_ka = nn_ka, n_va = nn_va;
         }
