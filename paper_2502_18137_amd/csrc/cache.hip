@@ -6,6 +6,7 @@ namespace sparge {
 namespace {
 
 constexpr int PLAN_THREADS = 1024;
+constexpr int DEAL = 8 * PLAN_THREADS;           // pages that change hands at a time
 constexpr int FILL_IN_PLAN = 4 * PLAN_THREADS;   // slots that the plan's one workgroup fills itself
 
 __device__ __forceinline__ int blocks_of(int tokens) { return (tokens + PAGE - 1) / PAGE; }
@@ -26,30 +27,41 @@ struct Sums {
 };
 
 // exclusive prefix of v over the workgroup's threads, and the total; lds: a Sums per wave
-__device__ __forceinline__ Sums up(const Sums& v, int lanes, int width) {
-    return {__shfl_up(v.push, lanes, width), __shfl_up(v.need, lanes, width), __shfl_up(v.tok, lanes, width)};
-}
 __device__ Sums scan(const Sums& v, Sums* lds, Sums& total) {
     constexpr int WAVES = PLAN_THREADS / 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Sums x = v;
-#pragma unroll 1
-    for (int s = 1; s < 64; s <<= 1) {
-        const Sums y = up(x, s, 64);
-        if (lane >= s) x.push += y.push, x.need += y.need, x.tok += y.tok;
-    }
+    static_assert(WAVES == 16, "a row of lanes holds the waves' sums");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+    Sums x = {scan_lanes(v.push), scan_lanes(v.need), scan_lanes(v.tok)};
     if (lane == 63) lds[wave] = x;
     __syncthreads();
-    Sums w = lds[lane % WAVES];
-#pragma unroll 1
-    for (int s = 1; s < WAVES; s <<= 1) {
-        const Sums y = up(w, s, WAVES);
-        if (lane % WAVES >= s) w.push += y.push, w.need += y.need, w.tok += y.tok;
-    }
-    total = {__shfl(w.push, WAVES - 1), __shfl(w.need, WAVES - 1), __shfl(w.tok, WAVES - 1)};
-    const Sums before = {__shfl(w.push, max(wave - 1, 0)), __shfl(w.need, max(wave - 1, 0)), __shfl(w.tok, max(wave - 1, 0))};
-    if (wave) x.push += before.push, x.need += before.need, x.tok += before.tok;
-    return {x.push - v.push, x.need - v.need, x.tok - v.tok};
+    const Sums w = lds[lane % WAVES], upto = {scan_lanes<16>(w.push), scan_lanes<16>(w.need), scan_lanes<16>(w.tok)};
+    total = {lane_value(upto.push, WAVES - 1), lane_value(upto.need, WAVES - 1), lane_value(upto.tok, WAVES - 1)};
+    x.push += lane_value(upto.push, wave) - lane_value(w.push, wave) - v.push;
+    x.need += lane_value(upto.need, wave) - lane_value(w.need, wave) - v.need;
+    x.tok += lane_value(upto.tok, wave) - lane_value(w.tok, wave) - v.tok;
+    return x;
+}
+
+// the largest value of the threads before (0 for the first, values >= 0); lds: an int per wave
+__device__ __forceinline__ int max_before(int v, int* lds) {
+    auto step = [&](auto ctrl, auto rows) {
+        v = max(v, __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false));
+    };
+    using all = std::integral_constant<int, 0xF>;
+    step(std::integral_constant<int, 0x111>{}, all{});
+    step(std::integral_constant<int, 0x112>{}, all{});
+    step(std::integral_constant<int, 0x114>{}, all{});
+    step(std::integral_constant<int, 0x118>{}, all{});
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (lane == 63) lds[wave] = v;
+    lds_barrier();
+    int before = __shfl_up(v, 1);
+    if (lane == 0) before = 0;
+    for (int w = 0; w < PLAN_THREADS / 64; ++w)
+        if (w < wave) before = max(before, lds[w]);
+    return before;
 }
 
 __device__ __forceinline__ void fill_slot(const sparge_cache& c, const int* cu, int total, int i, const int* held, int32_t* slots,
@@ -72,10 +84,14 @@ __device__ __forceinline__ void fill_slot(const sparge_cache& c, const int* cu, 
 __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c, const int32_t* __restrict__ new_len,
                                                                   const uint8_t* __restrict__ release, int n_slots, int32_t* cu,
                                                                   int32_t* slots, int32_t* req, int32_t* status) {
-    extern __shared__ int lds[];
-    int* push_at = lds;                 // prefix sums over the rows; then the rows' held tokens
+    extern __shared__ __align__(16) int lds[];   // over the rows: prefix sums of pages given up, pages taken, new tokens; held tokens
+    int* push_at = lds;
     int* need_at = lds + c.R;
     int* tok_at = lds + 2 * c.R;
+    int* held_of = lds + 3 * c.R;
+    int* top = lds + (c.R + 1) / 2 * 2 * 4;   // the stack's upper end after the pushes: page `pushed - 1 - a` in top[a], a < cached
+    int* map = top + DEAL;              // where rows begin
+    __shared__ int wave_max[PLAN_THREADS / 64];
     __shared__ Sums wave_sums[PLAN_THREADS / 64];
     __shared__ int all_flags;
     const int tid = threadIdx.x;
@@ -114,76 +130,77 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
         if (tid == 0) status[0] = flags, status[1] = n_free;
         return;
     }
+    const int pushed = static_cast<int>(total.push), needed = static_cast<int>(total.need), tokens = static_cast<int>(total.tok);
+    const int cached = min(min(pushed, needed), DEAL);
 #pragma unroll 1
     for (int r = r0; r < r1; ++r) {
-        push_at[r] = static_cast<int>(at.push), need_at[r] = static_cast<int>(at.need), tok_at[r] = static_cast<int>(at.tok);
+        const int len = c.length[r], n = new_len[r], held = release && release[r] ? 0 : len;
+        push_at[r] = static_cast<int>(at.push), need_at[r] = static_cast<int>(at.need), tok_at[r] = static_cast<int>(at.tok), held_of[r] = held;
         cu[r] = static_cast<int>(at.tok);
-        const int len = c.length[r], n = new_len[r];
-        const bool rel = release && release[r];
-        const int held = rel ? 0 : len;
-        at.push += rel ? blocks_of(len) : 0;
+        c.length[r] = held + n;
+        at.push += blocks_of(len) * (held != len);
         at.need += blocks_of(held + n) - blocks_of(held);
         at.tok += n;
     }
-    __syncthreads();
-    const int pushed = static_cast<int>(total.push), needed = static_cast<int>(total.need), tokens = static_cast<int>(total.tok);
+    lds_barrier();
     int32_t* stack = c.free_pages + n_free;
 #pragma unroll 1
     for (int pop = 0; pop < 2; ++pop) {
-        // Groups of 64 rows are dealt out over the waves (a group to several where there are few), a lane counts a row's pages in
-        // pieces of 64, and the wave takes the pieces one after the other, eight at a time on their way.  (Pages dealt out over
-        // the threads, each looking up its row, take 17 to 25 us where this takes PLAN_US: one compute unit's issue.)
+        // Pages are dealt out eight a thread, in the rows' order: every row writes its number where its pages begin, and the
+        // largest number up to a place is the place's row.  (One compute unit's issue is what bounds this: a search per page
+        // through the prefix sums takes 8 us, whole rows or pieces of them by waves 7, this 2, for the 9000 pages that 200 of
+        // 1000 rows give up.)
         const int* prefix = pop ? need_at : push_at;
-        const int n = pop ? needed : pushed, groups = (c.R + 63) / 64, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        constexpr int WAVES = PLAN_THREADS / 64;
-        const int log2 = groups > 1 ? min(4, 32 - __builtin_clz(groups - 1)) : 0, sharers = WAVES >> log2, share = wave >> log2;
+        const int n = pop ? needed : pushed;
 #pragma unroll 1
-        for (int g = wave & ((1 << log2) - 1); g < groups; g += 1 << log2) {
-            const int r = 64 * g + lane;
-            int count = 0, base = 0, first = 0;
-            if (r < c.R) {
-                base = prefix[r], count = (r + 1 < c.R ? prefix[r + 1] : n) - base;
-                if (pop) first = blocks_of(push_at[r]);
+        for (int c0 = 0; c0 < n; c0 += DEAL) {
+            int4* mine4 = reinterpret_cast<int4*>(map + 8 * tid);
+            mine4[0] = mine4[1] = make_int4(0, 0, 0, 0);
+            lds_barrier();
+#pragma unroll 1
+            for (int r = r0; r < r1; ++r) {
+                const int begin = prefix[r], end = r + 1 < c.R ? prefix[r + 1] : n;
+                if (begin < end && begin < c0 + DEAL && end > c0) map[max(begin - c0, 0)] = r + 1;
             }
-            const int pieces = (count + 63) / 64;
-            int upto = pieces;
-#pragma unroll 1
-            for (int s = 1; s < 64; s <<= 1) {
-                const int y = __shfl_up(upto, s);
-                if (lane >= s) upto += y;
-            }
-            const int all = __builtin_amdgcn_readlane(upto, 63);
-#pragma unroll 1
-            for (int k0 = 8 * share; k0 < all; k0 += 8 * sharers) {
-                int page[8];
-                int32_t* to[8];
+            lds_barrier();
+            int row[8];
+            *reinterpret_cast<int4*>(row) = mine4[0], *reinterpret_cast<int4*>(row + 4) = mine4[1];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    to[e] = nullptr;
-                    if (k0 + e >= all) continue;
-                    const int at = __builtin_popcountll(__ballot(upto <= k0 + e));   // the row's lane
-                    const int b = 64 * (k0 + e - __builtin_amdgcn_readlane(upto - pieces, at)) + lane;
-                    if (b >= __builtin_amdgcn_readlane(count, at)) continue;
-                    const int a = __builtin_amdgcn_readlane(base, at) + b;
-                    int32_t* entry = c.table + static_cast<long long>(64 * g + at) * c.max_blocks + __builtin_amdgcn_readlane(first, at) + b;
-                    int32_t* place = stack + (pop ? pushed - 1 - a : a);
-                    to[e] = pop ? entry : place;
-                    page[e] = *(pop ? place : entry);
+            for (int e = 1; e < 8; ++e) row[e] = max(row[e], row[e - 1]);
+            const int before = max_before(row[7], wave_max);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) row[e] = max(row[e], before);
+            // back to LDS: the wave's 512 pages again with neighbours in neighbouring lanes, for whole lines to and from memory
+            mine4[0] = *reinterpret_cast<int4*>(row), mine4[1] = *reinterpret_cast<int4*>(row + 4);
+            const int a0 = 512 * (tid >> 6) + (tid & 63);
+            int page[8], *entry[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int a = c0 + a0 + 64 * e, r = map[a0 + 64 * e] - 1;
+                entry[e] = nullptr;
+                if (a >= n) continue;
+                entry[e] = c.table + static_cast<long long>(r) * c.max_blocks + (a - prefix[r] + (pop ? blocks_of(held_of[r]) : 0));
+                if (!pop) page[e] = *entry[e];
+                else if (a < cached) page[e] = top[a];
+                else page[e] = stack[pushed - 1 - a];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int a = c0 + a0 + 64 * e;
+                if (!entry[e]) continue;
+                if (pop) {
+                    *entry[e] = page[e];
+                } else {
+                    stack[a] = page[e];
+                    if (pushed - 1 - a < cached) top[pushed - 1 - a] = page[e];
                 }
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (to[e]) *to[e] = page[e];
             }
         }
         if (pop) break;
-        __syncthreads();
-#pragma unroll 1
-        for (int r = r0; r < r1; ++r) {
-            const int held = release && release[r] ? 0 : c.length[r];
-            push_at[r] = held;
-            c.length[r] = held + new_len[r];
-        }
-        __syncthreads();
+        // What is taken now may be what was given up just now: it is passed on through LDS, so that nobody waits for the stack's
+        // stores, unless there are too many.  (Entries are written only after all that are given up have been read.)
+        if (min(pushed, needed) > cached) __syncthreads();
+        else lds_barrier();
     }
     if (tid == 0) {
         cu[c.R] = tokens;
@@ -192,14 +209,14 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
     }
     if (n_slots > FILL_IN_PLAN) return;
     __syncthreads();
-    for (int i = tid; i < n_slots; i += PLAN_THREADS) fill_slot(c, tok_at, tokens, i, push_at, slots, req);
+    for (int i = tid; i < n_slots; i += PLAN_THREADS) fill_slot(c, tok_at, tokens, i, held_of, slots, req);
 }
 
 // The slot map of a long step, from what the plan has written; a workgroup per 512 slots.
 constexpr int FILL_SLOTS = 512;
 __global__ __launch_bounds__(256) void cache_slots_kernel(sparge_cache c, int n_slots, const int32_t* __restrict__ cu,
                                                           int32_t* slots, int32_t* req) {
-    extern __shared__ int lds[];
+    extern __shared__ __align__(16) int lds[];
     int* held = lds + c.R;
     const int total = min(cu[c.R], n_slots);
     for (int r = threadIdx.x; r < c.R; r += 256) {
@@ -565,8 +582,9 @@ __global__ __launch_bounds__(256, 6) void cache_read_kernel(sparge_cache c, cons
 
 hipError_t launch_cache_plan(const sparge_cache& c, const int32_t* new_len, const uint8_t* release, int n_slots, int32_t* cu,
                              int32_t* slots, int32_t* req, int32_t* status, hipStream_t st) {
-    hipLaunchKernelGGL(cache_plan_kernel, dim3(1), dim3(PLAN_THREADS), 3 * c.R * sizeof(int), st, c, new_len, release, n_slots, cu,
-                       slots, req, status);
+    const int lds = (c.R + 1) / 2 * 2 * 4 + 2 * DEAL;   // ints: the rows (16-byte aligned for what follows), the stack's end, the map
+    hipLaunchKernelGGL(cache_plan_kernel, dim3(1), dim3(PLAN_THREADS), lds * sizeof(int), st, c, new_len, release, n_slots, cu, slots, req,
+                       status);
     if (n_slots > FILL_IN_PLAN)
         hipLaunchKernelGGL(cache_slots_kernel, dim3((n_slots + FILL_SLOTS - 1) / FILL_SLOTS), dim3(256), 2 * c.R * sizeof(int), st, c,
                            n_slots, cu, slots, req);

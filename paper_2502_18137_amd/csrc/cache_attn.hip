@@ -117,11 +117,7 @@ struct Joint {                          // workspace
 // exclusive prefix of v over the 256 threads and the total; lds: 4 values
 __device__ __forceinline__ u64 prefix(u64 v, u64* lds, u64& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    u64 upto = v;
-    for (int s = 1; s < 64; s <<= 1) {
-        const u64 x = __shfl_up(upto, s);
-        if (lane >= s) upto += x;
-    }
+    u64 upto = scan_lanes(static_cast<long long>(v));
     if (lane == 63) lds[wave] = upto;
     __syncthreads();
     total = 0;
@@ -550,11 +546,6 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
         it = nx;
         have = n_have;
     }
-}
-
-// A barrier for what goes through LDS: loads from memory that are on their way stay on it (__syncthreads waits for them).
-__device__ __forceinline__ void lds_barrier() {
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // ---- many query rows: four waves share the blocks --------------------------------------------------------------------
