@@ -972,8 +972,10 @@ __device__ __forceinline__ void join(const sparge_cache& c, const CacheAttn& a, 
     const JoinDesc d = ws.desc[(bid * 4 + wave) / WAVES];
     if (d.n_parts == 0) return;
     const int Gp = cut_of(a.H / c.H_kv, ROWS).Gp, me = (d.part - d.first) * WAVES + wave % WAVES, workers = (d.n_parts - 1) * WAVES;
+    // as many groups of lanes as bring an item's parts in with one round trip, while its waves have chunks enough
     if (d.n_parts <= 4) join_item<D, DT, ROWS, 1>(d, me, workers, Gp, a, O, ws);
-    else join_item<D, DT, ROWS, 8>(d, me, workers, Gp, a, O, ws);
+    else if (d.n_parts <= 64) join_item<D, DT, ROWS, 8>(d, me, workers, Gp, a, O, ws);
+    else join_item<D, DT, ROWS, 32>(d, me, workers, Gp, a, O, ws);
 }
 // the first n_wide workgroups take the wide kernel's parts, the others the narrow one's
 template <int D, int DT>
