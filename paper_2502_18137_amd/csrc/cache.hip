@@ -488,32 +488,30 @@ __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, co
 
 // ---- read-back ---------------------------------------------------------------------------------------------------
 
-// value = code amax / 127 (+ shift), in 64 bits and rounded once to fp32, then to 16 bits where asked for.  A workgroup takes the
-// runs of consecutive slots of one page inside its window of `window` (a power of two up to 64) slots, K (blockIdx.z 0) or V
-// of one kv head, from the page's 16-byte pieces as they lie: K a token's 16 channels, V a channel of 16 tokens, whose
-// neighbours write the tokens' neighbouring channels.
-template <int OUT>
-__device__ __forceinline__ void put(void* out, long long at, const float* y, int n) {   // n = 1, 2 or a multiple of 4 (8) values
+// value = code amax / 127 (+ shift) rounded once to fp32, then to 16 bits where asked for.  With a shift, and where amax is next to
+// the ends of fp32's range, it is formed in 64 bits.  Otherwise step = amax / 127 is split into its upper 17 bits, whose
+// products with a code are exact, and the rest: value = code upper + code rest in one fma, off by 2^-41 of itself before its rounding.
+// That is the exact quotient's rounding: N / 127 (N = code times amax's 24 bits) is no nearer than 2^-32 of itself to what lies half
+// way between two floats, unless it is just there, and then 127 divides amax's bits and both parts are exact.
+template <int OUT, int N>
+__device__ __forceinline__ void put(void* out, const float (&y)[N]) {   // 4, 8 or 16 bytes
     if constexpr (OUT == SPARGE_F32) {
-        float* p = static_cast<float*>(out) + at;
-        if (n == 1) *p = y[0];
-        else if (n == 2) *reinterpret_cast<float2*>(p) = make_float2(y[0], y[1]);
-        else for (int e = 0; e < n; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+        __builtin_memcpy(__builtin_assume_aligned(out, 4 * N), y, 4 * N);
     } else {
-        uint16_t* p = static_cast<uint16_t*>(out) + at;
-        if (n == 1) *p = cvt_to16<OUT>(y[0]);
-        else if (n == 2) *reinterpret_cast<uint32_t*>(p) = cvt_to16<OUT>(y[0]) | static_cast<uint32_t>(cvt_to16<OUT>(y[1])) << 16;
-        else for (int e = 0; e < n; e += 8) {
-            uint32_t w[4];
-            for (int k = 0; k < 4; ++k) w[k] = cvt_to16<OUT>(y[e + 2 * k]) | static_cast<uint32_t>(cvt_to16<OUT>(y[e + 2 * k + 1])) << 16;
-            *reinterpret_cast<uint4*>(p + e) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        uint16_t w[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) w[e] = cvt_to16<OUT>(y[e]);
+        __builtin_memcpy(__builtin_assume_aligned(out, 2 * N), w, 2 * N);
     }
 }
+// A workgroup takes the runs of consecutive slots of one page inside its window of `window` (a power of two up to 64) slots, K
+// (blockIdx.z 0) or V of one kv head.  Bound by its bytes; what counts is that a store instruction covers whole lines: a thread takes
+// 16 bytes' worth of a token's channels of K (4 or 8 codes; with 16 codes a thread as the pieces lie the stores are 64 bytes
+// apart, and fp32 took 294 us in the place of 231 for 50k tokens of 16 heads of 128 channels) and 1 or 2 channels of V's 16 tokens.
 template <int D, int OUT>
 __global__ __launch_bounds__(256, 6) void cache_read_kernel(sparge_cache c, const int32_t* __restrict__ slots,
                                                          const int32_t* __restrict__ req, int n_slots, int window, void* K, void* V) {
-    constexpr int CV = D / 64;
+    constexpr int EL = OUT == SPARGE_F32 ? 4 : 2, CV = D / 64, KCH = 16 / EL;   // bytes of an output; channels of a thread, V and K
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), hk = blockIdx.y, i0 = blockIdx.x * window;
     const bool is_v = blockIdx.z != 0;
     int my_slot = -1, my_row = 0;
@@ -534,46 +532,68 @@ __global__ __launch_bounds__(256, 6) void cache_read_kernel(sparge_cache c, cons
         const int slot = __builtin_amdgcn_readlane(my_slot, first), r = __builtin_amdgcn_readlane(my_row, first);
         const int page = slot / PAGE, off = slot % PAGE;
         const long long at = static_cast<long long>(page) * c.H_kv + hk;
-        const uint4* codes = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(is_v ? c.v : c.k) + at * PAGE * D);
-        const double step = static_cast<double>((is_v ? c.v_amax : c.k_amax)[at]) / 127.0;
-        const long long out0 = (static_cast<long long>(i0 + first - off) * c.H_kv + hk) * D;   // of the page's token 0
-        auto value = [&](const uint32_t (&w)[4], int e) {
-            return static_cast<double>(static_cast<int>((w[e >> 2] >> (8 * (e & 3))) & 0xFFu) - 128) * step;
-        };
+        const uint8_t* codes = static_cast<const uint8_t*>(is_v ? c.v : c.k) + at * PAGE * D;
+        const float amax = (is_v ? c.v_amax : c.k_amax)[at];
+        const double step = static_cast<double>(amax) / 127.0;
+        const float* shift = c.k_shift && !is_v ? c.k_shift + (static_cast<long long>(r) * c.H_kv + hk) * D : nullptr;
+        // outputs: a uniform address for the page's token t, and the thread's own bytes from there (4 MiB at most)
+        const uint32_t row_bytes = c.H_kv * D * EL;
+        char* out0 = static_cast<char*>(is_v ? V : K) + (static_cast<long long>(i0 + first - off) * c.H_kv + hk) * (D * EL);
+        auto in_run = [&](int t) { return t >= off && t < off + n; };
+        constexpr int LPT = D / KCH, STEP = 256 / LPT;   // K: threads per token, tokens of the workgroup at a time
+        const int k_tok = threadIdx.x / LPT, k_ch = (threadIdx.x % LPT) * KCH;
+        uint32_t w[D / 16];   // K: KCH codes of each of its tokens; V: 16 codes of each of its channels
         if (is_v) {
-            uint32_t w[CV][4];
 #pragma unroll
             for (int p = 0; p < CV; ++p) {
                 const int ch = CV * lane + p;
-                const uint4 raw = codes[(ch >> 4) * 64 + (ch & 15) + 16 * wave];
-                w[p][0] = raw.x, w[p][1] = raw.y, w[p][2] = raw.z, w[p][3] = raw.w;
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int t = 16 * (e >> 2) + 4 * wave + (e & 3);
-                if (t < off || t >= off + n) continue;
-                float y[CV];
-#pragma unroll
-                for (int p = 0; p < CV; ++p) y[p] = static_cast<float>(value(w[p], e));
-                put<OUT>(V, out0 + static_cast<long long>(t) * c.H_kv * D + CV * lane, y, CV);
-                __builtin_amdgcn_sched_barrier(0);
+                const uint4 raw = reinterpret_cast<const uint4*>(codes)[(ch >> 4) * 64 + (ch & 15) + 16 * wave];
+                w[4 * p] = raw.x, w[4 * p + 1] = raw.y, w[4 * p + 2] = raw.z, w[4 * p + 3] = raw.w;
             }
         } else {
-            const float* shift = c.k_shift ? c.k_shift + (static_cast<long long>(r) * c.H_kv + hk) * D : nullptr;
 #pragma unroll
-            for (int p = 0; p < CV; ++p) {
-                const int piece = wave + 4 * p, t = 16 * (piece / CV) + (lane & 15), ch = 64 * (piece % CV) + 16 * (lane >> 4);
-                if (t < off || t >= off + n) continue;
-                const uint4 raw = codes[piece * 64 + lane];
-                const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-                float y[16];
+            for (int p = 0; p < PAGE / STEP; ++p)
+                if (in_run(p * STEP + k_tok))
+                    __builtin_memcpy(w + KCH / 4 * p, __builtin_assume_aligned(codes + k_byte(p * STEP + k_tok, k_ch, D), KCH), KCH);
+        }
+        auto write = [&](auto value) {   // value(code, the channel's index of the thread)
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) asm volatile("" : "+v"(w[k]));   // unpacked here, not ahead of the branch
+            auto code = [](uint32_t word, int e) { return static_cast<int>((word >> (8 * e)) & 0xFFu) - 128; };
+            if (is_v) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    y[e] = static_cast<float>(shift ? value(w, e) + static_cast<double>(shift[ch + e]) : value(w, e));
-                    if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+                    const int t = 16 * (e >> 2) + 4 * wave + (e & 3);
+                    if (!in_run(t)) continue;
+                    float y[CV];
+#pragma unroll
+                    for (int p = 0; p < CV; ++p) y[p] = value(code(w[4 * p + (e >> 2)], e & 3), p);
+                    put<OUT>(out0 + static_cast<long long>(t) * row_bytes + static_cast<uint32_t>(CV * EL * lane), y);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                put<OUT>(K, out0 + static_cast<long long>(t) * c.H_kv * D + ch, y, 16);
+            } else {
+#pragma unroll
+                for (int p = 0; p < PAGE / STEP; ++p) {
+                    const int t = p * STEP + k_tok;
+                    if (!in_run(t)) continue;
+                    float y[KCH];
+#pragma unroll
+                    for (int e = 0; e < KCH; ++e) y[e] = value(code(w[KCH / 4 * p + e / 4], e & 3), e);
+                    put<OUT>(out0 + static_cast<long long>(p * STEP) * row_bytes + (k_tok * row_bytes + static_cast<uint32_t>(k_ch * EL)), y);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
+        };
+        if (!shift && amax >= 0x1p-90f && amax <= 0x1p127f) {
+            const float upper = __uint_as_float(__float_as_uint(static_cast<float>(step)) & ~0x7Fu);
+            const float rest = static_cast<float>(step - static_cast<double>(upper));
+            write([&](int q, int) { return __builtin_fmaf(static_cast<float>(q), rest, static_cast<float>(q) * upper); });
+        } else {
+            float sh[KCH] = {};
+            if (shift)
+#pragma unroll
+                for (int e = 0; e < KCH; e += 4) *reinterpret_cast<float4*>(sh + e) = *reinterpret_cast<const float4*>(shift + k_ch + e);
+            write([&](int q, int e) { return static_cast<float>(static_cast<double>(q) * step + static_cast<double>(sh[e])); });
         }
     }
 }
