@@ -288,15 +288,28 @@ __device__ __forceinline__ uint32_t workgroup_max(uint32_t v, uint32_t* lds) {
     return __builtin_amdgcn_readfirstlane(max(max(lds[0], lds[1]), max(lds[2], lds[3])));
 }
 
+// The kv head and the first slot of a workgroup of a grid (windows, kv heads, ..): the heads of a window run together, as their tokens and
+// pages lie together.  (Windows first, all workgroups that run at one time want the same 256 bytes of every 4 KB of 16 heads'
+// tokens: 65k of them took 234 us to append in the place of 190 and 306 to read to fp32 in the place of 247.)
+__device__ __forceinline__ void heads_first(int window, int& hk, int& i0) {
+    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
+    hk = id % gridDim.y;
+    i0 = id / gridDim.y * window;
+}
+
 // A workgroup quantizes one kv head's K or V of every page that begins to get tokens inside its window of `window` (a power of two
 // up to 64) slots: the open page's older tokens from the tail, the new ones from the call's tensor.  Bound by its bytes: a
 // thread holds what makes whole 16-byte pieces of the page (K: 16 channels of a token; V: a channel of 16 tokens), loads and
-// stores are coalesced and nothing goes through LDS but the maxima.  Where a page gets few tokens that do not raise its amax
+// stores are coalesced and nothing goes through LDS but the maxima: 65k tokens of 16 heads of 128 channels, 805 MB, in 190 us, 4.2 TB/s,
+// where a large copy reaches 5.  (K and V of a page in one workgroup, their loads together: 69 us in the place of 57 for
+// 29k tokens of 8 heads.)  Where a page gets few tokens that do not raise its amax
 // (decoding: all but one of t + 1 at the t-th token of a page), the older codes are what they were and only the new ones are
 // written; the tail's amax per token tells without reading the tail.
 // The row's first page also stores the tokens of the row's last page if that stays open (after it has read the older
 // ones, which lie in the same place).
-constexpr int FEW = 8;   // tokens of a page whose codes are written by themselves
+// FEW: tokens of a page up to which their codes are written by themselves (200 rows of 32 heads, all by themselves against none: 34 us
+// against 45 for one token a row, 42 against 47 for 2, 46 against 61 for 8).
+constexpr int FEW = 8;
 template <int D, int DT>
 __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, const uint16_t* __restrict__ K,
                                                            const uint16_t* __restrict__ V, int n_slots, int window, long long k_sn,
@@ -306,12 +319,13 @@ __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, co
     constexpr int LPR = D / 8, RPS = 256 / LPR;   // threads per token of 8 channels each, tokens at a time
     constexpr int CV = D / 64;                    // V: channels per thread; K: pieces per thread
     __shared__ uint32_t lds_max[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hk = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int hk, i0;
+    heads_first(window, hk, i0);
     const bool is_v = blockIdx.z != 0;
     const uint16_t* x = is_v ? V + hk * v_sh : K + hk * k_sh;
     const long long sn = is_v ? v_sn : k_sn;
 
-    const int i0 = blockIdx.x * window;
     int my_slot = -1, my_row = -1, my_prev = -1;
     if (lane < window && i0 + lane < n_slots) {
         my_slot = slots[i0 + lane];
@@ -507,12 +521,15 @@ __device__ __forceinline__ void put(void* out, const float (&y)[N]) {   // 4, 8 
 // A workgroup takes the runs of consecutive slots of one page inside its window of `window` (a power of two up to 64) slots, K
 // (blockIdx.z 0) or V of one kv head.  Bound by its bytes; what counts is that a store instruction covers whole lines: a thread takes
 // 16 bytes' worth of a token's channels of K (4 or 8 codes; with 16 codes a thread as the pieces lie the stores are 64 bytes
-// apart, and fp32 took 294 us in the place of 231 for 50k tokens of 16 heads of 128 channels) and 1 or 2 channels of V's 16 tokens.
+// apart: 294 us in the place of 231 for 50k tokens of 16 heads of 128 channels to fp32, now 195, 5.2 TB/s) and 1 or 2 channels of V's
+// 16 tokens.
 template <int D, int OUT>
 __global__ __launch_bounds__(256, 6) void cache_read_kernel(sparge_cache c, const int32_t* __restrict__ slots,
                                                          const int32_t* __restrict__ req, int n_slots, int window, void* K, void* V) {
     constexpr int EL = OUT == SPARGE_F32 ? 4 : 2, CV = D / 64, KCH = 16 / EL;   // bytes of an output; channels of a thread, V and K
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), hk = blockIdx.y, i0 = blockIdx.x * window;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+    int hk, i0;
+    heads_first(window, hk, i0);
     const bool is_v = blockIdx.z != 0;
     int my_slot = -1, my_row = 0;
     if (lane < window && i0 + lane < n_slots) {
@@ -611,18 +628,21 @@ hipError_t launch_cache_plan(const sparge_cache& c, const int32_t* new_len, cons
     return hipGetLastError();
 }
 
-// Slots per workgroup of the append and the read-back: a page's worth where there are that many, down to one (which may be a page
-// of its own) where there are few: a workgroup takes its window's pages one after the other.
-static int window_of(int n_slots, int heads) {
+// Slots per workgroup of the append and the read-back: a page's worth where that makes enough workgroups, down to one (which may be a
+// page of its own) where it does not: a workgroup takes its window's pages one after the other.  Enough is 1024 for the
+// append (with 512, 200 rows of one token and 32 heads take 46 us in the place of 36, 128 rows and 8 heads 10.1 in the place of 9.4; with 4096, a
+// piece of a prompt 13 in the place of 7.7: most workgroups have nothing to do) and 512 for the read-back, whose runs end
+// at windows (with 1024, 1k tokens of 4 heads take 7.8 us in the place of 5.6).
+static int window_of(int n_slots, int heads, int groups) {
     int window = 64;
-    while (window > 1 && static_cast<long long>(n_slots / window) * heads < 512) window /= 2;
+    while (window > 1 && static_cast<long long>(n_slots / window) * heads < groups) window /= 2;
     return window;
 }
 
 hipError_t launch_cache_append(const sparge_cache& c, const void* K, const void* V, int n_slots, long long k_sn, long long k_sh,
                                long long v_sn, long long v_sh, const int32_t* cu, const int32_t* slots, const int32_t* req,
                                hipStream_t st) {
-    const int window = window_of(n_slots, c.H_kv);
+    const int window = window_of(n_slots, c.H_kv, 1024);
     const dim3 grid((n_slots + window - 1) / window, c.H_kv, 2);
     const uint16_t *k = static_cast<const uint16_t*>(K), *v = static_cast<const uint16_t*>(V);
 #define APPEND(D, DT) \
@@ -638,7 +658,7 @@ hipError_t launch_cache_append(const sparge_cache& c, const void* K, const void*
 
 hipError_t launch_cache_read(const sparge_cache& c, const int32_t* slots, const int32_t* req, int n_slots, int out_dtype, void* K,
                              void* V, hipStream_t st) {
-    const int window = window_of(n_slots, c.H_kv);
+    const int window = window_of(n_slots, c.H_kv, 512);
     const dim3 grid((n_slots + window - 1) / window, c.H_kv, 2);
 #define READ(D, OUT) hipLaunchKernelGGL((cache_read_kernel<D, OUT>), grid, dim3(256), 0, st, c, slots, req, n_slots, window, K, V)
     if (c.d == 64) {
