@@ -111,7 +111,7 @@ __device__ __forceinline__ RowInfo uniform(RowInfo x) {
 struct Joint {                          // workspace
     JoinDesc* desc;                     // [parts]
     float* ml;                          // [2 parts][rows of a tile][2] reference and sum of a row's part
-    float* o;                           // [2 parts][rows of a tile][d]
+    float* o;                           // [2 parts][rows of a tile][d] mean of the values over the part's keys
 };
 
 // exclusive prefix of v over the 256 threads and the total; lds: 4 values
@@ -259,12 +259,16 @@ __device__ __forceinline__ float nan_f() { return __uint_as_float(0x7FC00000u); 
 struct VScale {
     float ref = 0.f, f_log2, f_inv;
 
+    // a / b from their significands and exponents: reciprocals of subnormals, and subnormal reciprocals, are flushed
+    static __device__ __forceinline__ float ratio(float a, float b) {
+        return __builtin_ldexpf(__builtin_amdgcn_frexp_mantf(a) * __builtin_amdgcn_rcpf(__builtin_amdgcn_frexp_mantf(b)),
+                                __builtin_amdgcn_frexp_expf(a) - __builtin_amdgcn_frexp_expf(b));
+    }
     // -> what O has to be multiplied with first (1: nothing)
     __device__ __forceinline__ float take(float va) {
         float down = 1.0f;
-        if (va > SV_SLACK * ref) down = ref * __builtin_amdgcn_rcpf(va), ref = va;
-        float f = va * __builtin_amdgcn_rcpf(ref);
-        if (va < SV_LEAST * ref || va == 0.f) f = SV_LEAST;   // (a block of zeros has codes 0 whatever the factor)
+        if (va > SV_SLACK * ref) down = ratio(ref, va), ref = va;
+        const float f = fmaxf(ratio(va, ref), SV_LEAST);   // (a block of zeros has codes 0 whatever the factor, NaN where ref is 0, too)
         f_log2 = __builtin_amdgcn_logf(f) + P_UP_LOG2, f_inv = __builtin_amdgcn_rcpf(f) * 0x1p-8f;
         return down;
     }
@@ -311,25 +315,27 @@ __device__ __forceinline__ void softmax(v4f (&s)[4], float cq, const VScale& v, 
     for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = static_cast<_Float16>(w[e]);
 }
 
-// A tile's rows, whole (divided by their sums) or as a part.
+// What O has to be multiplied with first and then by V's reference scale (one after the other: neither product leaves fp32's range
+// where the result does not).
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : (1.0f / (127.0f * 256.0f)) / l; }
+// A tile's rows, divided by their sums, as results or as a part's.
 template <int NV, int DT>
-__device__ __forceinline__ void store_whole(const v4f (&o)[NV], float l, float o_scale, uint16_t* out) {
-    const float inv = o_scale / l;
+__device__ __forceinline__ void store_whole(const v4f (&o)[NV], float inv, float ref, uint16_t* out) {
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
         uint16_t h[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = l == 0.f ? 0 : cvt_to16<DT>(o[n][e] * inv);
+        for (int e = 0; e < 4; ++e) h[e] = cvt_to16<DT>(o[n][e] * inv * ref);
         uint2 w;
         __builtin_memcpy(&w, h, 8);
         *reinterpret_cast<uint2*>(out + 16 * n) = w;
     }
 }
 template <int NV>
-__device__ __forceinline__ void store_part(const v4f (&o)[NV], float m, float l, float o_scale, const Joint& ws, long long at) {
+__device__ __forceinline__ void store_part(const v4f (&o)[NV], float m, float l, float inv, float ref, const Joint& ws, long long at) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int n = 0; n < NV; ++n) *reinterpret_cast<v4f*>(ws.o + at * (16 * NV) + 16 * n + 4 * (lane >> 4)) = o[n] * o_scale;
+    for (int n = 0; n < NV; ++n) *reinterpret_cast<v4f*>(ws.o + at * (16 * NV) + 16 * n + 4 * (lane >> 4)) = o[n] * inv * ref;
     if (lane < 16) ws.ml[2 * at] = m, ws.ml[2 * at + 1] = l;
 }
 
@@ -536,11 +542,11 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
         }
         l = sum_groups(l);
         if (mine_valid) {
-            const float o_scale = vs.ref * (1.0f / (127.0f * 256.0f));
+            const float inv = inverse(l);
             if (it.b0 == 0 && it.b1 == it.blocks) {
-                store_whole<NV, DT>(o, l, o_scale, O + my_token * a.o_sn + my_head * a.o_sh + 4 * (lane >> 4));
+                store_whole<NV, DT>(o, inv, vs.ref, O + my_token * a.o_sn + my_head * a.o_sh + 4 * (lane >> 4));
             } else {
-                store_part<NV>(o, m, l, o_scale, ws, static_cast<long long>(2 * part + (it.b0 > 0 ? 0 : 1)) * NARROW_ROWS + (lane & 15));
+                store_part<NV>(o, m, l, inv, vs.ref, ws, static_cast<long long>(2 * part + (it.b0 > 0 ? 0 : 1)) * NARROW_ROWS + (lane & 15));
             }
         }
         it = nx;
@@ -843,8 +849,7 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
 
         l += other<32>(l);
         if (valid) {
-            const float o_scale = vs.ref * (1.0f / (127.0f * 256.0f));
-            const float inv = o_scale / l;
+            const float inv = inverse(l);
             uint16_t* out = O + token * a.o_sn + hd * a.o_sh + 4 * half;
             const long long row_at = static_cast<long long>(2 * part + (x0 > 0 ? 0 : 1)) * WIDE_ROWS + row;
 #pragma unroll
@@ -853,16 +858,16 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
                 for (int e = 0; e < 4; ++e) {   // channels 32 n + 8 e + 4 half + 0..3
                     v4f y;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) y[k] = o[n][4 * e + k];
+                    for (int k = 0; k < 4; ++k) y[k] = o[n][4 * e + k] * inv * vs.ref;
                     if (whole) {
                         uint16_t h[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) h[k] = l == 0.f ? 0 : cvt_to16<DT>(y[k] * inv);
+                        for (int k = 0; k < 4; ++k) h[k] = cvt_to16<DT>(y[k]);
                         uint2 w;
                         __builtin_memcpy(&w, h, 8);
                         *reinterpret_cast<uint2*>(out + 32 * n + 8 * e) = w;
                     } else {
-                        *reinterpret_cast<v4f*>(ws.o + row_at * D + 32 * n + 8 * e + 4 * half) = y * o_scale;
+                        *reinterpret_cast<v4f*>(ws.o + row_at * D + 32 * n + 8 * e + 4 * half) = y;
                     }
                 }
             if (!whole && half == 0) ws.ml[2 * row_at] = m, ws.ml[2 * row_at + 1] = l;
@@ -909,7 +914,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_both_kernel(sparge_cache c,
 
 // Joins items that several parts hold, each in its parts' order.  An item's rows are cut into chunks of channels, which the waves
 // of the parts that begin inside the item deal out among them.  A wave's lanes take 4 channels each of 256 / PG, and the
-// PG groups of lanes every PG-th part, up to eight of them in one round trip to memory.
+// PG groups of lanes every PG-th part, up to eight of them in one round trip to memory.  What is joined are means of the values, with
+// weights that add up to 1: no sum leaves fp32's range where the result does not.
 template <int D, int DT, int ROWS, int PG>
 __device__ __forceinline__ void join_item(const JoinDesc& d, int me, int workers, int Gp, const CacheAttn& a, uint16_t* O, const Joint& ws) {
     constexpr int LANES = 64 / PG;
@@ -937,28 +943,28 @@ __device__ __forceinline__ void join_item(const JoinDesc& d, int me, int workers
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = fmaxf(top, pm[e]);
-            const float down = __builtin_amdgcn_exp2f(m - top);
-            l *= down, o *= down, m = top;
+            const float before = l * __builtin_amdgcn_exp2f(m - top);
+            l = before, m = top;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float w = __builtin_amdgcn_exp2f(pm[e] - top);
-                l += pl[e] * w;
-                o += po[e] * w;
-            }
+            for (int e = 0; e < 8; ++e) pl[e] *= __builtin_amdgcn_exp2f(pm[e] - top), l += pl[e];
+            const float inv = l == 0.f ? 0.f : __builtin_amdgcn_rcpf(l);
+            o *= before * inv;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o += po[e] * (pl[e] * inv);
         }
 #pragma unroll
         for (int x = LANES; x < 64; x <<= 1) {
             const float om = __shfl_xor(m, x), ol = __shfl_xor(l, x), top = fmaxf(m, om);
-            const float wa = __builtin_amdgcn_exp2f(m - top), wb = __builtin_amdgcn_exp2f(om - top);
-            l = l * wa + ol * wb;
+            const float la = l * __builtin_amdgcn_exp2f(m - top), lb = ol * __builtin_amdgcn_exp2f(om - top);
+            l = la + lb, m = top;
+            const float inv = l == 0.f ? 0.f : __builtin_amdgcn_rcpf(l);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = o[e] * wa + __shfl_xor(o[e], x) * wb;
-            m = top;
+            for (int e = 0; e < 4; ++e) o[e] = o[e] * (la * inv) + __shfl_xor(o[e], x) * (lb * inv);
         }
         if (there && grp == 0) {
             uint16_t h[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = l == 0.f ? 0 : cvt_to16<DT>(o[e] / l);
+            for (int e = 0; e < 4; ++e) h[e] = cvt_to16<DT>(o[e]);
             uint2 w;
             __builtin_memcpy(&w, h, 8);
             *reinterpret_cast<uint2*>(O + static_cast<long long>(d.token + tok) * a.o_sn + static_cast<long long>(d.head + g) * a.o_sh + ch) = w;
