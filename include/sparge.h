@@ -366,7 +366,7 @@ int sparge_cache_read(const sparge_cache* cache, const int32_t* slots, const int
  * cu[R] stay as they were.  sm_scale <= 0 selects 1/sqrt(d).
  * Products are 16-bit with fp32 sums; the codes enter them exactly (integers up to 127 in fp16), Q as it is (bf16 times a
  * power of two per row, in fp16), the weights rounded to fp16.  The result does not depend on timing.
- * The workspace (256-byte aligned) carries nothing between calls; calls that may overlap need one each.
+ * O must not overlap Q.  The workspace (256-byte aligned) carries nothing between calls; calls that may overlap need one each.
  */
 int sparge_cache_attn_workspace_bytes(const sparge_cache* cache, int H, size_t* bytes /* host, out */);
 int sparge_cache_attn(const sparge_cache* cache, const void* Q, int n_slots, int H, int64_t q_stride_n, int64_t q_stride_h,

@@ -52,3 +52,91 @@ def test_values_over_bf16s_range(sp, G, new):
         plan = m.step(n, tokens=(K, V))
     m.check_stored()
     relative_check(m, plan, 2 * G, m.queries(2 * G))
+
+
+@pytest.mark.parametrize("G", [1, 4, 17])
+def test_all_rows_there_can_be(sp, G):
+    """4096 rows of few keys, some of them empty: more rows than parts, parts that hold several rows"""
+    m = Model(sp, 4096, 1, 64, 4200, 2, dtype="bf16", seed=30 + G)
+    m.step(m.rng.integers(0, 4, size=4096).tolist())
+    plan = m.step((m.rng.random(4096) < 0.9).astype(int).tolist())
+    m.check_attn(plan, G)
+    plan = m.step((m.rng.integers(0, 40, size=4096) == 0).astype(int).tolist(), pad=5)
+    m.check_attn(plan, G, pad=5)
+
+
+@pytest.mark.parametrize("G,new", [(1, 1), (3, 40)])
+def test_as_many_heads_as_there_can_be(sp, G, new):
+    Hkv = 128 // G
+    m = Model(sp, 2, Hkv, 64, 20, 8, dtype="fp16", seed=33, shift=True)
+    m.step([130, 5])
+    m.check_stored()
+    m.check_attn(m.step([new, new]), Hkv * G)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("G,new", [(2, [1, 1, 1]), (2, [30, 1, 0]), (40, [2, 1, 3])])
+def test_everything_at_once(sp, G, new, causal):
+    """a block mask, tokens inside a projection's output, rows behind the last token, a shift, a softmax scale"""
+    m = Model(sp, 3, 2, 128, 40, 12, dtype="bf16", seed=34, shift=True)
+    m.step([500, 63, 1], pad=9, fused=3)
+    plan = m.step(new, pad=21, fused=2)
+    m.check_stored()
+    mask = (m.rng.random((3, 2, 12)) < 0.5).astype(np.uint8)
+    m.check_attn(plan, 2 * G, causal=causal, mask=mask, scale=0.3, pad=21, fused=1)
+
+
+def test_two_calls_at_once(sp):
+    """the same and different queries over one cache on two streams, a workspace each"""
+    import torch
+    m = Model(sp, 4, 2, 128, 400, 130, dtype="bf16", seed=35)
+    m.step([8000, 100, 3000, 64])
+    plan = m.step([1, 20, 1, 3])
+    q = [m.gpu(m.queries(8)) for _ in range(2)]
+    want = [sp.sparge_cache_attn(m.cache, x, plan) for x in q]
+    n = sp.sparge_cache_attn_workspace_bytes(m.cache, 8)
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    out = [[torch.zeros_like(x) for _ in range(4)] for x in q]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for k in range(4):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                sp.sparge_cache_attn(m.cache, q[i], plan, ws=ws[i], out=out[i][k])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o in out[i]:
+            assert torch.equal(o, want[i])
+
+
+def test_a_step_without_tokens(sp):
+    """rows that are only padding, or none at all: nothing changes, nothing is written"""
+    import torch
+    m = Model(sp, 3, 2, 64, 20, 4, dtype="fp16", seed=36)
+    m.step([70, 0, 5])
+    plan = m.step([0, 0, 0], pad=6)
+    m.check_stored()
+    m.check_attn(plan, 4, pad=6)
+    plan = m.step([0, 0, 0])
+    m.check_stored()
+    assert sp.sparge_cache_attn(m.cache, m.gpu(np.zeros((0, 4, 64))), plan).shape == (0, 4, 64)
+    k, v = sp.sparge_cache_read(m.cache, m.i32([]))
+    assert k.shape == v.shape == (0, 2, 64)
+    m.step([0, 0, 0], release=[1, 0, 1])
+    assert m.book.length == [0, 0, 0]
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "fp16"), (128, "bf16")])
+def test_reads_in_every_order(sp, d, dtype):
+    """the same slot again and again, runs forwards and backwards, single ones, runs over a page's end, more slots than tokens"""
+    import torch
+    m = Model(sp, 2, 3, d, 10, 4, dtype=dtype, seed=37)
+    m.step([200, 131])
+    at = lambda r, t: m.book.table[r, t // 64] * 64 + t % 64
+    seq = [(0, t) for t in range(200)] + [(0, t) for t in range(199, 150, -1)] + [(1, 7)] * 70 + [(1, t) for t in range(60, 70)]
+    seq += [(int(r), int(t)) for r, t in zip(m.rng.integers(0, 2, 300), m.rng.integers(0, 131, 300))]
+    k, v = sp.sparge_cache_read(m.cache, m.i32([int(at(r, t)) for r, t in seq]), dtype=torch.float32)
+    kept = [m.stored(r)[:2] for r in range(2)]
+    for i, x in enumerate((k, v)):
+        want = np.stack([kept[r][i][t] for r, t in seq]).astype(np.float32)
+        assert np.array_equal(x.cpu().numpy(), want)
