@@ -788,11 +788,13 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
             const float from = vs.f_log2 - m;
             float sum = 0.f;
             v8h pf[4], v[4];
-            auto weights = [&](int u, int e) {   // two of the eight of step u; the sum takes them as they are rounded, two an instruction
+            auto weights = [&](int u, int e) {   // two of the eight of step u
 #pragma unroll
-                for (int k = e; k < e + 2; ++k)
-                    pf[u][k] = static_cast<_Float16>(__builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + k], cq, from)));
-                sum = __builtin_amdgcn_fdot2(v2h{pf[u][e], pf[u][e + 1]}, v2h{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+                for (int k = e; k < e + 2; ++k) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + k], cq, from));
+                    sum += w;
+                    pf[u][k] = static_cast<_Float16>(w);
+                }
                 asm volatile("" : "+v"(sum));   // here, not all of them behind the last product
             };
             auto operand = [&](int x) { return lds_v[buf][((x % NC) * 4 + x / NC) * 64 + lane]; };
