@@ -792,7 +792,7 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
 #pragma unroll
                 for (int k = e; k < e + 2; ++k) {
                     const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + k], cq, from));
-                    sum += w;
+                    sum += w;   // before its rounding: w carries V's factor, which may be small
                     pf[u][k] = static_cast<_Float16>(w);
                 }
                 asm volatile("" : "+v"(sum));   // here, not all of them behind the last product
