@@ -42,8 +42,8 @@ __device__ Sums scan(const Sums& v, Sums* lds, Sums& total) {
     return x;
 }
 
-// the largest value of the threads before (0 for the first, values >= 0); lds: an int per wave
-__device__ __forceinline__ int max_before(int v, int* lds) {
+// the largest of a wave's values up to each lane (values >= 0), through DPP row moves
+__device__ __forceinline__ int max_lanes(int v) {
     auto step = [&](auto ctrl, auto rows) {
         v = max(v, __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false));
     };
@@ -54,6 +54,11 @@ __device__ __forceinline__ int max_before(int v, int* lds) {
     step(std::integral_constant<int, 0x118>{}, all{});
     step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});
     step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});
+    return v;
+}
+// the largest value of the threads before (0 for the first, values >= 0); lds: an int per wave
+__device__ __forceinline__ int max_before(int v, int* lds) {
+    v = max_lanes(v);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (lane == 63) lds[wave] = v;
     lds_barrier();
@@ -279,13 +284,20 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
     return __builtin_amdgcn_perm(cd, ab, 0x05040100u);
 }
 
-// the largest of 256 threads' values; lds: 4
-__device__ __forceinline__ uint32_t workgroup_max(uint32_t v, uint32_t* lds) {
-    for (int s = 1; s < 64; s <<= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), s)));
+// the largest of 256 threads' values below 2^31, N of them at once; lds: 4 N
+template <int N>
+__device__ __forceinline__ void workgroup_max(uint32_t (&v)[N], uint32_t* lds) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = max_lanes(v[k]);
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 63) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) lds[4 * k + (threadIdx.x >> 6)] = v[k];
+    }
     __syncthreads();
-    return __builtin_amdgcn_readfirstlane(max(max(lds[0], lds[1]), max(lds[2], lds[3])));
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        v[k] = __builtin_amdgcn_readfirstlane(max(max(lds[4 * k], lds[4 * k + 1]), max(lds[4 * k + 2], lds[4 * k + 3])));
 }
 
 // The kv head and the first slot of a workgroup of a grid (windows, kv heads, ..): the heads of a window run together, as their tokens and
@@ -318,7 +330,7 @@ __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, co
                                                            const int32_t* __restrict__ req) {
     constexpr int LPR = D / 8, RPS = 256 / LPR;   // threads per token of 8 channels each, tokens at a time
     constexpr int CV = D / 64;                    // V: channels per thread; K: pieces per thread
-    __shared__ uint32_t lds_max[4];
+    __shared__ uint32_t lds_max[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int hk, i0;
     heads_first(window, hk, i0);
@@ -365,7 +377,9 @@ __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, co
 #pragma unroll
                 for (int e = 0; e < 8; ++e) top = max(top, abs_bits(y[e]));
             }
-            const uint32_t old = workgroup_max(before, lds_max), now = workgroup_max(top, lds_max);
+            uint32_t tops[2] = {before, top};
+            workgroup_max(tops, lds_max);
+            const uint32_t old = tops[0], now = tops[1];
             if (off == 0 || old >= now) {
                 done = true;
                 const uint32_t amax = max(old, now);
@@ -445,7 +459,9 @@ __global__ __launch_bounds__(256, 6) void cache_append_kernel(sparge_cache c, co
                     }
                 top = abs_bits(cvt16<DT>(max(two[0], two[1])));
             }
-            top = workgroup_max(top, lds_max);
+            uint32_t tops[1] = {top};
+            workgroup_max(tops, lds_max);
+            top = tops[0];
             const Quantizer q(top);
 #pragma unroll
             for (int p = 0; p < CV; ++p)
@@ -630,7 +646,7 @@ hipError_t launch_cache_plan(const sparge_cache& c, const int32_t* new_len, cons
 
 // Slots per workgroup of the append and the read-back: a page's worth where that makes enough workgroups, down to one (which may be a
 // page of its own) where it does not: a workgroup takes its window's pages one after the other.  Enough is 1024 for the
-// append (with 512, 200 rows of one token and 32 heads take 46 us in the place of 36, 128 rows and 8 heads 10.1 in the place of 9.4; with 4096, a
+// append (with 512, 200 rows of one token and 32 heads take 46 us in the place of 33, 128 rows and 8 heads 10.1 in the place of 8.8; with 4096, a
 // piece of a prompt 13 in the place of 7.7: most workgroups have nothing to do) and 512 for the read-back, whose runs end
 // at windows (with 1024, 1k tokens of 4 heads take 7.8 us in the place of 5.6).
 static int window_of(int n_slots, int heads, int groups) {

@@ -361,10 +361,13 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
     const int per = (c.R + 255) / 256;
     auto blocks_in = [&](const RowInfo& x) { return x.n ? (x.len + PAGE - 1) / PAGE : 0; };
     auto length_of = [&](const RowInfo& x) { return static_cast<u64>(x.tiles) * heads * blocks_in(x); };
-    u64 mine = 0;
     Line line;
+    const int r0 = tid * per, r1 = min(r0 + per, c.R);
+    RowInfo row0 = {0, 0, 0, 0, 0};
+    if (r0 < r1) row0 = row_info(c, a, cut, which, r0);
+    u64 mine = length_of(row0);
 #pragma unroll 1
-    for (int r = tid * per; r < min((tid + 1) * per, c.R); ++r) mine += length_of(row_info(c, a, cut, which, r));
+    for (int r = r0 + 1; r < r1; ++r) mine += length_of(row_info(c, a, cut, which, r));
     const u64 before = prefix(mine, sh.sums, line.total);
     line.total = uniform(line.total);
     line.log2 = line.total >> NARROW_LOG2 ? NARROW_LOG2 : line.total ? 63 - __builtin_clzll(line.total) : 0;
@@ -374,8 +377,8 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
         const u64 at = line.begin(bid * 4 + w);
         if (bid * 4 + w < parts && before <= at && at < before + mine) {
             u64 rem = at - before;
-            int r = tid * per;
-            RowInfo x = row_info(c, a, cut, which, r);
+            int r = r0;
+            RowInfo x = row0;
 #pragma unroll 1
             while (rem >= length_of(x) && r < c.R - 1) {
                 rem -= length_of(x);
@@ -399,7 +402,6 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
     int b_next = static_cast<int>(rem - in_row * row_blocks);
     int head = info.tiles ? static_cast<int>(quotient(in_row, info.tiles)) : 0;
     int tile = static_cast<int>(in_row) - head * info.tiles;
-    bool first_item = true;
 
     struct Item {
         RowInfo x;
@@ -425,15 +427,6 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
         const int take = static_cast<int>(min(static_cast<u64>(row_blocks - b_next), left));
         it.b1 = b_next += take;
         left -= take;
-        if (first_item) {
-            first_item = false;
-            JoinDesc d = NO_JOIN;
-            const int g0 = it.gpart * NARROW_ROWS;
-            if (it.b0 > 0)
-                d = boundary(line, part, lo - it.b0, lo - it.b0 + it.blocks, info.first + tile * cut.TT, it.ntok, it.kh * cut.G + g0,
-                             min(cut.Gp, cut.G - g0));
-            if (lane == 0) ws.desc[part] = d;
-        }
         return true;
     };
 
@@ -467,15 +460,20 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
     Item it;
     bool have = next_item(it), more = false;
     int block = 0, page = 0, at = 0;
-    if (!have && lane == 0) ws.desc[part] = NO_JOIN;
+    JoinDesc join = NO_JOIN;
     if (have) {
         open(it);
+        const int g0 = it.gpart * NARROW_ROWS;   // (worked out while the table is on its way)
+        if (it.b0 > 0)
+            join = boundary(line, part, lo - it.b0, lo - it.b0 + it.blocks, it.x.first + it.tile * cut.TT, it.ntok, it.kh * cut.G + g0,
+                            min(cut.Gp, cut.G - g0));
         more = blocks.next(c, it.kh, block, page, at);
         if (more) {
             load_k(page, it.kh);
             load_v(page, it.kh);
         }
     }
+    if (lane == 0) ws.desc[part] = join;
     while (have) {
         v8h qf[KS];
         const float qs = a.scale_log2 * convert_q<D, DT>(q_raw, qf);
@@ -607,10 +605,13 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
     // ---- this workgroup's part of the line, in keys
     const int per = (c.R + 255) / 256;
     auto length_of = [&](const RowInfo& x) { return sum_vis(x, cut, a.causal, x.tiles); };
-    u64 mine = 0;
     Line line;
+    const int r0 = tid * per, r1 = min(r0 + per, c.R);
+    RowInfo row0 = {0, 0, 0, 0, 0};
+    if (r0 < r1) row0 = row_info(c, a, cut, which, r0);
+    u64 mine = length_of(row0) * heads;
 #pragma unroll 1
-    for (int r = tid * per; r < min((tid + 1) * per, c.R); ++r) mine += length_of(row_info(c, a, cut, which, r)) * heads;
+    for (int r = r0 + 1; r < r1; ++r) mine += length_of(row_info(c, a, cut, which, r)) * heads;
     const u64 before = prefix(mine, sh.sums, line.total);
     line.total = uniform(line.total);
     // parts of at least two blocks; neighbours on the line, which share pages, are neighbours on an XCD
@@ -625,8 +626,8 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
     const u64 lo = line.begin(part);
     if (before <= lo && lo < before + mine) {
         u64 rem = lo - before;
-        int r = tid * per;
-        RowInfo x = row_info(c, a, cut, which, r);
+        int r = r0;
+        RowInfo x = row0;
 #pragma unroll 1
         while (rem >= length_of(x) * heads && r < c.R - 1) {
             rem -= length_of(x) * heads;
