@@ -131,6 +131,7 @@ __device__ __forceinline__ u64 prefix(u64 v, u64* lds, u64& total) {
 // a / b, both below 2^52.  (Kernels that run for a few microseconds wait for their own instructions: the 64-bit division that the
 // compiler would put in its place has 130 of them.)
 __device__ __forceinline__ u64 quotient(u64 a, u64 b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
     u64 q = static_cast<u64>(static_cast<double>(a) / static_cast<double>(b));
     while (q * b > a) --q;
     while ((q + 1) * b <= a) ++q;
@@ -345,9 +346,8 @@ __device__ __forceinline__ void store_part(const v4f (&o)[NV], float m, float l,
 // waves on a compute unit; and it looks ahead over the end of an item, so that the next one's table, queries and first block
 // come while the last block of this one is worked on.
 struct NarrowShared {
-    u64 sums[4], rem[4];
-    int row[4];
-    RowInfo info[4];
+    u64 sums[4], before[256];           // per thread: places on the line before its rows, the first of these
+    RowInfo info[256];
 };
 template <int D, int DT>
 __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a, Rows which, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
@@ -372,31 +372,27 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
     line.total = uniform(line.total);
     line.log2 = line.total >> NARROW_LOG2 ? NARROW_LOG2 : line.total ? 63 - __builtin_clzll(line.total) : 0;
     const int parts = line.total ? 1 << line.log2 : 0, part = bid * 4 + wave;
-#pragma unroll 1
-    for (int w = 0; w < 4; ++w) {
-        const u64 at = line.begin(bid * 4 + w);
-        if (bid * 4 + w < parts && before <= at && at < before + mine) {
-            u64 rem = at - before;
-            int r = r0;
-            RowInfo x = row0;
-#pragma unroll 1
-            while (rem >= length_of(x) && r < c.R - 1) {
-                rem -= length_of(x);
-                x = row_info(c, a, cut, which, ++r);
-            }
-            sh.row[w] = r, sh.rem[w] = rem, sh.info[w] = x;
-        }
-    }
+    sh.before[tid] = before, sh.info[tid] = row0;
     __syncthreads();
     if (part >= parts) {
         if (lane == 0) ws.desc[part] = NO_JOIN;
         return;
     }
-    // the next item's first block to take: row, of all heads' tiles the tile's number, block
-    int r = uniform(sh.row[wave]);
-    RowInfo info = uniform(sh.info[wave]);
+    // the next item's first block to take: row, of all heads' tiles the tile's number, block.  The row is one of the last thread's that
+    // has no more than the part's beginning before it.
+    const u64 lo = line.begin(part);
+    int t = -1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t += __builtin_popcountll(__ballot(sh.before[4 * lane + e] <= lo));
+    int r = t * per;
+    u64 rem = lo - uniform(sh.before[t]);
+    RowInfo info = uniform(sh.info[t]);
+#pragma unroll 1
+    while (rem >= length_of(info) && r < c.R - 1) {
+        rem -= length_of(info);
+        info = uniform(row_info(c, a, cut, which, ++r));
+    }
     int row_blocks = blocks_in(info);
-    const u64 lo = line.begin(part), rem = uniform(sh.rem[wave]);
     u64 left = line.begin(part + 1) - lo;                     // blocks that this wave still has to take
     const u64 in_row = row_blocks ? quotient(rem, row_blocks) : 0;
     int b_next = static_cast<int>(rem - in_row * row_blocks);
