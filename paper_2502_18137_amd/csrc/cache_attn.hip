@@ -347,7 +347,10 @@ __device__ __forceinline__ void store_part(const v4f (&o)[NV], float m, float l,
 
 // Bound by the pages' bytes: a wave keeps the next block's K and V on their way while it works on one, 16 KB (d = 128), eight
 // waves on a compute unit; and it looks ahead over the end of an item, so that the next one's table, queries and first block
-// come while the last block of this one is worked on.
+// come while the last block of this one is worked on.  160 rows of 5000 to 33000 keys, 8 kv heads of 128 channels, 4.9 GB: 832 us, 5.8 TB/s,
+// where a large copy reaches 5.0; 64 rows of 300 to 9000 keys, 0.33 GB: 65 us.  (Three waves a SIMD, whose registers spill: 116 us
+// in the place of 100.)  A lone row of 500 keys takes 7.6 us, a chain of latencies: the rows' sums, the table, the
+// queries, the page.
 struct NarrowShared {
     u64 sums[4], before[256];           // per thread: places on the line before its rows, the first of these
     RowInfo info[256];
@@ -588,6 +591,10 @@ __device__ __forceinline__ float convert_q32(const uint4 (&raw)[D / 16], v8h (&q
     }
 }
 
+// Bound by the issue of vector instructions (the conversions, the exponentials) beside the products, at the clock that the power limit leaves: of a
+// compute unit's cycles the vector ALU issues in 61 %, the matrix pipe works in 42 %, LDS moves data in two thirds.  3 rows of 700 to 2048 tokens
+// over 4000 to 30000 keys, 32 heads over 8: 540 GFLOP in 650 us with the join, 0.83 PFLOP/s, where a large bf16 product reaches
+// 1.14.  (64 query rows a wave, one workgroup a compute unit: 1147 us in the place of 917.)
 // Four waves share the blocks: their codes are converted once per workgroup into LDS, in the operand order of the 32x32x16 MFMA
 // (two buffers, one barrier a block; the raw bytes of the block after the next are on their way meanwhile), and every wave
 // reads them for its own 32 query rows.  In that MFMA's accumulators a lane owns one query (lane % 32) and, of every 16 keys,
@@ -1039,12 +1046,15 @@ hipError_t launch_cache_attn(const sparge_cache& c, const CacheAttn& a, const vo
     Joint j[2];
     for (int k = 0; k < 2; ++k)
         j[k] = {reinterpret_cast<JoinDesc*>(p + x.desc[k]), reinterpret_cast<float*>(p + x.ml[k]), reinterpret_cast<float*>(p + x.o[k])};
-    // How many tokens each row adds is not known here.  Groups beyond a wave's 16 rows are the wide kernel's.  Up to 16 tokens
-    // more than rows (one each, and what pads a batch), or up to half a wave's rows on average, are taken for decoding: the
-    // narrow kernel alone, which gives the right result for longer rows, too.  A single row of more is the wide kernel's; else both
-    // run side by side, each on its rows.
+    // How many tokens each row adds is not known here.  Groups beyond a wave's 16 rows are the wide kernel's (16 rows, 8 queries a head: narrow
+    // 26 us, wide 36; 16 queries: 30 and 38).  Up to 16 tokens more than rows (one each, and what pads a batch), or up to half a
+    // wave's rows on average, are taken for decoding: the narrow kernel alone, which gives the right result for longer rows, too
+    // (64 rows of 300 to 9000 keys, 4 queries a head: 1 token 72 us, wide 113, both 74; 2 tokens 78, 111, 80; 8 tokens 129, 123, 124).
+    // More of them in a single row are the wide kernel's (9000 keys, 4 queries a head: 2 tokens narrow 17.8 us, wide 18.1; 4 tokens
+    // 22.3 and 18.6; 8 tokens 27.2 and 18.9); else both run side by side, each on its rows (8 rows of 1 to 600 tokens: both 140 us,
+    // wide 142, narrow 268).
     const long long G = a.H / c.H_kv;
-    const bool few = a.n_slots <= c.R + 16 || a.n_slots * G <= NARROW_ROWS / 2 * c.R;
+    const bool few = a.n_slots <= (c.R > 1 ? c.R + 16 : 1) || a.n_slots * G <= NARROW_ROWS / 2 * c.R;
     const bool narrow = G <= NARROW_ROWS && (few || c.R > 1), wide = G > NARROW_ROWS || !few;
 #define RUN(D, DT) launch<D, DT>(c, a, narrow, wide, Q, O, j, st)
     if (c.d == 64) {
