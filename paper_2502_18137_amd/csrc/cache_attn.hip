@@ -606,7 +606,8 @@ struct WideShared {
     RowInfo info;
     __align__(16) v8h k[2][2 * D / 16 * 64], v[2][D / 32 * 4 * 64];
 };
-template <int D, int DT>
+// TWO: weights in two parts, as in the narrow kernel.
+template <int D, int DT, bool TWO>
 __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, Rows which, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
                                      const Joint& ws, int bid, WideShared<D>& sh) {
     constexpr int KS = D / 16, NC = D / 32, RAW = D / 64;   // steps of K Q^T, channel tiles, 16-byte pieces of K (of V) per thread
@@ -802,13 +803,14 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
             }
             const float from = vs.f_log2 - m;
             float sum = 0.f;
-            v8h pf[4], v[4];
+            v8h pf[4], rest[4], v[4];
             auto weights = [&](int u, int e) {   // two of the eight of step u
 #pragma unroll
                 for (int k = e; k < e + 2; ++k) {
                     const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + k], cq, from));
                     sum += w;   // before its rounding: w carries V's factor, which may be small
                     pf[u][k] = static_cast<_Float16>(w);
+                    if constexpr (TWO) rest[u][k] = static_cast<_Float16>(w - static_cast<float>(pf[u][k]));
                 }
                 asm volatile("" : "+v"(sum));   // here, not all of them behind the last product
             };
@@ -822,6 +824,7 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
             for (int x = 0; x < 4 * NC; ++x) {
                 const int u = x / NC, n = x % NC;
                 o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x & 3], pf[u], o[n], 0, 0, 0);
+                if constexpr (TWO) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x & 3], rest[u], o[n], 0, 0, 0);
                 if (x + 4 < 4 * NC) v[x & 3] = operand(x + 4);
                 if (u < 3) {
 #pragma unroll
@@ -908,12 +911,12 @@ __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache 
     __shared__ NarrowShared sh;
     narrow<D, DT>(c, a, ALL_ROWS, Q, O, ws, blockIdx.x, sh);
 }
-template <int D, int DT>
+template <int D, int DT, bool TWO>
 __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c, CacheAttn a, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O, Joint ws) {
     __shared__ WideShared<D> sh;
-    wide<D, DT>(c, a, ALL_ROWS, Q, O, ws, blockIdx.x, sh);
+    wide<D, DT, TWO>(c, a, ALL_ROWS, Q, O, ws, blockIdx.x, sh);
 }
-template <int D, int DT>
+template <int D, int DT, bool TWO>
 __global__ __launch_bounds__(256, 2) void cache_attn_both_kernel(sparge_cache c, CacheAttn a, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
                                                                  Joint ws_wide, Joint ws_narrow) {
     __shared__ union Shared {
@@ -921,7 +924,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_both_kernel(sparge_cache c,
         WideShared<D> wide;
         NarrowShared narrow;
     } sh;
-    if (blockIdx.x < WIDE_WGS) wide<D, DT>(c, a, MANY_ROWS, Q, O, ws_wide, blockIdx.x, sh.wide);
+    if (blockIdx.x < WIDE_WGS) wide<D, DT, TWO>(c, a, MANY_ROWS, Q, O, ws_wide, blockIdx.x, sh.wide);
     else narrow<D, DT>(c, a, FEW_ROWS, Q, O, ws_narrow, blockIdx.x - WIDE_WGS, sh.narrow);
 }
 
@@ -1029,8 +1032,17 @@ template <int D, int DT>
 void launch(const sparge_cache& c, const CacheAttn& a, bool narrow, bool wide, const void* Qp, void* Op, const Joint (&j)[2], hipStream_t st) {
     const uint16_t* Q = static_cast<const uint16_t*>(Qp);
     uint16_t* O = static_cast<uint16_t*>(Op);
-    if (narrow && wide) hipLaunchKernelGGL((cache_attn_both_kernel<D, DT>), dim3(WIDE_WGS + NARROW_WGS), dim3(256), 0, st, c, a, Q, O, j[0], j[1]);
-    else if (wide) hipLaunchKernelGGL((cache_attn_wide_kernel<D, DT>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, Q, O, j[0]);
+    auto many = [&](auto two) {
+        constexpr bool TWO = decltype(two)::value;
+        if (narrow) hipLaunchKernelGGL((cache_attn_both_kernel<D, DT, TWO>), dim3(WIDE_WGS + NARROW_WGS), dim3(256), 0, st, c, a, Q, O, j[0], j[1]);
+        else hipLaunchKernelGGL((cache_attn_wide_kernel<D, DT, TWO>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, Q, O, j[0]);
+    };
+    // The second part of fp16's weights, where reading pages counts for more than products: up to 64 query rows a row of the cache on
+    // average (32 rows of one token and 32 heads: 29.9 us in the place of 28.8; prompts of 1000 tokens would take 840 us in the
+    // place of 652, and theirs are many rows: 1.25 times the error of the results' own rounding).
+    const bool two = DT == SPARGE_F16 && static_cast<long long>(a.n_slots) * (a.H / c.H_kv) <= WIDE_ROWS / 2 * c.R;
+    if (wide && two) many(std::bool_constant<DT == SPARGE_F16>{});
+    else if (wide) many(std::false_type{});
     else hipLaunchKernelGGL((cache_attn_narrow_kernel<D, DT>), dim3(NARROW_WGS), dim3(256), 0, st, c, a, Q, O, j[1]);
     const int n_wide = wide ? WIDE_WGS : 0, n_narrow = narrow ? NARROW_WGS : 0;
     hipLaunchKernelGGL((cache_join_kernel<D, DT>), dim3(n_wide + n_narrow), dim3(256), 0, st, c, a, n_wide, O, j[0], j[1]);
