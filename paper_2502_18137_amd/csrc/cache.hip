@@ -648,7 +648,7 @@ hipError_t launch_cache_plan(const sparge_cache& c, const int32_t* new_len, cons
 // page of its own) where it does not: a workgroup takes its window's pages one after the other.  Enough is 1024 for the
 // append (with 512, 200 rows of one token and 32 heads take 46 us in the place of 33, 128 rows and 8 heads 10.1 in the place of 8.8; with 4096, a
 // piece of a prompt 13 in the place of 7.7: most workgroups have nothing to do) and 512 for the read-back, whose runs end
-// at windows (with 1024, 1k tokens of 4 heads take 7.8 us in the place of 5.6).
+// at windows (with 1024, 374 tokens of 4 heads take 7.8 us in the place of 5.6).
 static int window_of(int n_slots, int heads, int groups) {
     int window = 64;
     while (window > 1 && static_cast<long long>(n_slots / window) * heads < groups) window /= 2;
