@@ -140,3 +140,21 @@ def test_reads_in_every_order(sp, d, dtype):
     for i, x in enumerate((k, v)):
         want = np.stack([kept[r][i][t] for r, t in seq]).astype(np.float32)
         assert np.array_equal(x.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("G,new", [(4, 1), (2, 6), (20, 1), (3, 20)])
+def test_fp16_results_are_off_by_their_own_rounding(sp, G, new):
+    """Up to 64 query rows a row, weights keep 22 bits: the error's norm is that of rounding the exact results to fp16 (half a step, 2^-11, at
+    most; 2^-12.3 of the results in the mean) but for terms of some 2^-18 of them (scores and sums in fp32), which add 1 % in
+    quadrature; 10 % is taken.  (Weights of one part, 2^-12.3 too, would add 20 to 60 %.)"""
+    m = Model(sp, 4, 2, 128, 140, 40, dtype="fp16", seed=40 + G)
+    m.step([2000, 130, 700, 1500])
+    plan = m.step([new] * 4)
+    q = m.queries(2 * G)
+    got = sp.sparge_cache_attn(m.cache, m.gpu(q), plan).double().cpu().numpy()
+    want = np.zeros_like(got)
+    for r in range(4):
+        k, v, _, _ = m.stored(r)
+        rows = slice(new * r, new * (r + 1))
+        want[rows] = co.attend(q[rows], k, v, len(k) - new, True, None, None)[0]
+    assert np.linalg.norm(got - want) <= 1.1 * np.linalg.norm(m.round16(want) - want)
