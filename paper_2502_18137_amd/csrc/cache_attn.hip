@@ -4,8 +4,10 @@
 // block's scales sk, sv: q_i . k_j = sk (q_i . a_j) and v_j = sv b_j.  Both products run on the 16-bit MFMA with the codes as
 // fp16 integers (exact), S^T = A Q^T and O^T = B^T P^T, so that a lane owns one query (lane % 16) and four keys of every
 // sixteen, and P goes from the accumulators of the first product to the operand of the second without leaving the lane:
-// the pages' byte order is made for that.  sk enters the exponent; sv enters p before it is rounded, relative to the
-// largest sv so far, to which O is kept relative.
+// the pages' byte order is made for that.  Both scales enter the exponent.  A query keeps two references: m, the largest score
+// so far, for the sum of the weights, and mo, the largest score + log2 sv, for O: the weights that meet V's codes are
+// exp2(score + log2 sv - mo), so that what fp16 rounds away is small beside what counts for this query most, whatever the sizes of V
+// in blocks that it gives no weight.
 //
 // The query rows of one row of the cache are its new tokens times the G heads that share a kv head.  Two kernels:
 //   rows of at most 16 query rows (decoding): the work is reading pages.  A wave takes blocks by itself, operands come
@@ -26,11 +28,11 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef unsigned long long u64;
 
 constexpr float FAR = -1e30f;          // reference of a row that has seen no key
-constexpr float SLACK = 6.0f;          // log2: how far a row's maximum may run ahead of the reference inside exp2
-constexpr float SV_SLACK = 2.0f;       // how far a block's V scale may exceed the one that O is relative to
-constexpr float P_UP_LOG2 = 8.0f;      // p is at most 2^6, its factor sv ratio at most 2: p x ratio x 2^8 <= 2^15 in fp16, and
-                                       // weights down to 2^-33 of the largest are not lost
-constexpr float SV_LEAST = 0x1p-60f;   // smaller ratios (and blocks of zeros) count as this: below every rounding beside sv_ref
+constexpr float SLACK = 6.0f;          // log2: how far a row's maxima may run ahead of their references inside exp2
+constexpr float W_UP = 9.0f;           // log2: weights are at most 2^(6 + 9) in fp16; the largest is 2^9 or more, and one of 2^-34 of it is
+                                       // not lost
+constexpr float W_LEAST = 60.0f;       // log2: a block whose largest weight would be less than 2^-60 (small V, zeros) is taken as if it were
+                                       // that: 0 in fp16, and the sum of the weights keeps it
 
 constexpr int NARROW_ROWS = 16, NARROW_WGS = 512, NARROW_LOG2 = 11;   // two workgroups per compute unit, a part per wave
 constexpr int WIDE_ROWS = 128, WIDE_WGS = 512, WIDE_LOG2 = 9;         // a part per workgroup
@@ -256,30 +258,22 @@ __device__ __forceinline__ float convert_q(const uint4 (&raw)[D / 32], v8h (&qf)
 __device__ __forceinline__ bool not_finite(float ka, float va) { return !(ka < INFINITY && va < INFINITY); }
 __device__ __forceinline__ float nan_f() { return __uint_as_float(0x7FC00000u); }
 
-// V's scale of a block against the one that O is relative to: the factor's log2 (with P_UP_LOG2) and inverse.
-struct VScale {
-    float ref = 0.f, f_log2, f_inv;
+// log2 of a block's V amax (-inf for zeros), subnormal ones too, which v_log_f32 takes for 0
+__device__ __forceinline__ float log2_of(float va) {
+    return __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(va)) + static_cast<float>(__builtin_amdgcn_frexp_expf(va));
+}
+// What is added to a row's scores of a block to make the exponents of its weights; top: the largest score.
+__device__ __forceinline__ float weight_log2(float v_log2, float mo, float top) {
+    return fmaxf(v_log2 - mo + W_UP, -W_LEAST - fmaxf(top, FAR));
+}
+// The block's sum of weights back in the units of l.
+__device__ __forceinline__ float weight_back(float add, float m) { return __builtin_amdgcn_exp2f(-add - m); }
 
-    // a / b from their significands and exponents: reciprocals of subnormals, and subnormal reciprocals, are flushed
-    static __device__ __forceinline__ float ratio(float a, float b) {
-        return __builtin_ldexpf(__builtin_amdgcn_frexp_mantf(a) * __builtin_amdgcn_rcpf(__builtin_amdgcn_frexp_mantf(b)),
-                                __builtin_amdgcn_frexp_expf(a) - __builtin_amdgcn_frexp_expf(b));
-    }
-    // -> what O has to be multiplied with first (1: nothing)
-    __device__ __forceinline__ float take(float va) {
-        float down = 1.0f;
-        if (va > SV_SLACK * ref) down = ratio(ref, va), ref = va;
-        const float f = fmaxf(ratio(va, ref), SV_LEAST);   // (a block of zeros has codes 0 whatever the factor, NaN where ref is 0, too)
-        f_log2 = __builtin_amdgcn_logf(f) + P_UP_LOG2, f_inv = __builtin_amdgcn_rcpf(f) * 0x1p-8f;
-        return down;
-    }
-};
-
-// One tile's softmax step on a block's scores s (keys 16 t + 4 (lane / 16) + e): the weights times V's factor as operand pf,
-// the row's reference m and sum l, O scaled where the reference moves.  last: the last key of the block that the row sees,
+// One tile's softmax step on a block's scores s (keys 16 t + 4 (lane / 16) + e): the weights with V's scale as operand pf, the row's
+// references m and mo and sum l, O and l scaled where the references move.  last: the last key of the block that the row sees,
 // less 4 (lane / 16); looked at only if `masked`.  pf[2], pf[3], where asked for: what the weights' rounding left.
 template <int NV, int NP>
-__device__ __forceinline__ void softmax(v4f (&s)[4], float cq, const VScale& v, bool masked, int last, float& m, float& l,
+__device__ __forceinline__ void softmax(v4f (&s)[4], float cq, float v_log2, bool masked, int last, float& m, float& mo, float& l,
                                         v4f (&o)[NV], v8h (&pf)[NP]) {
     if (cq == 0.f) cq = 1e-37f;   // a block of zeros: -inf stays what it is and becomes a weight of 0
     if (masked) {
@@ -295,23 +289,23 @@ __device__ __forceinline__ void softmax(v4f (&s)[4], float cq, const VScale& v, 
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, s[t][e]);
     top = max_groups(top) * cq;
-    if (__any(top > m + SLACK)) {
-        const float to = fmaxf(m, top), down = __builtin_amdgcn_exp2f(m - to);
-        m = to;
-        l *= down;
+    if (__any(top > m + SLACK || top + v_log2 > mo + SLACK)) {
+        const float to = fmaxf(m, top), o_to = fmaxf(mo, top + v_log2), down = __builtin_amdgcn_exp2f(mo - o_to);
+        l *= __builtin_amdgcn_exp2f(m - to);
+        m = to, mo = o_to;
 #pragma unroll
         for (int n = 0; n < NV; ++n) o[n] *= down;
     }
     float w[16];
-    const float from = v.f_log2 - m;
+    const float add = weight_log2(v_log2, mo, top);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[4 * t + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], cq, from));
+        for (int e = 0; e < 4; ++e) w[4 * t + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], cq, add));
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) sum += w[e];
-    l += sum * v.f_inv;
+    l += sum * weight_back(add, m);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         pf[e >> 3][e & 7] = static_cast<_Float16>(w[e]);
@@ -319,27 +313,41 @@ __device__ __forceinline__ void softmax(v4f (&s)[4], float cq, const VScale& v, 
     }
 }
 
-// What O has to be multiplied with first and then by V's reference scale (one after the other: neither product leaves fp32's range
-// where the result does not).
-__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : (1.0f / (127.0f * 256.0f)) / l; }
+// A row's O over its sum: times `by`, then 2^up.  (One after the other: neither leaves fp32's range where the result does not.)
+struct Mean {
+    float by;
+    int up;
+
+    __device__ __forceinline__ Mean(float l, float m, float mo) {
+        const float e = fminf(fmaxf(mo - m - W_UP, -400.0f), 400.0f), whole = floorf(e);   // (-400: a result of 0)
+        by = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(e - whole) * (1.0f / 127.0f) / l;
+        up = static_cast<int>(whole);
+    }
+    __device__ __forceinline__ float operator()(float o) const { return __builtin_ldexpf(o * by, up); }
+};
 // A tile's rows, divided by their sums, as results or as a part's.
 template <int NV, int DT>
-__device__ __forceinline__ void store_whole(const v4f (&o)[NV], float inv, float ref, uint16_t* out) {
+__device__ __forceinline__ void store_whole(const v4f (&o)[NV], const Mean& mean, uint16_t* out) {
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
         uint16_t h[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = cvt_to16<DT>(o[n][e] * inv * ref);
+        for (int e = 0; e < 4; ++e) h[e] = cvt_to16<DT>(mean(o[n][e]));
         uint2 w;
         __builtin_memcpy(&w, h, 8);
         *reinterpret_cast<uint2*>(out + 16 * n) = w;
     }
 }
 template <int NV>
-__device__ __forceinline__ void store_part(const v4f (&o)[NV], float m, float l, float inv, float ref, const Joint& ws, long long at) {
+__device__ __forceinline__ void store_part(const v4f (&o)[NV], const Mean& mean, float m, float l, const Joint& ws, long long at) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int n = 0; n < NV; ++n) *reinterpret_cast<v4f*>(ws.o + at * (16 * NV) + 16 * n + 4 * (lane >> 4)) = o[n] * inv * ref;
+    for (int n = 0; n < NV; ++n) {
+        v4f y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = mean(o[n][e]);
+        *reinterpret_cast<v4f*>(ws.o + at * (16 * NV) + 16 * n + 4 * (lane >> 4)) = y;
+    }
     if (lane < 16) ws.ml[2 * at] = m, ws.ml[2 * at + 1] = l;
 }
 
@@ -483,8 +491,7 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
         const int my_token = out_token, my_head = out_head;
         const bool mine_valid = valid;
         v4f o[NV];
-        float m = FAR, l = 0.f;
-        VScale vs;
+        float m = FAR, mo = FAR, l = 0.f;
 #pragma unroll
         for (int n = 0; n < NV; ++n) o[n] = {0.f, 0.f, 0.f, 0.f};
         Item nx;
@@ -522,17 +529,12 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
             if (more) {
                 const bool bad = not_finite(ka, va);
                 if (bad) ka = va = 0.f;
-                const float down = vs.take(va);
-                if (down != 1.0f) {
-#pragma unroll
-                    for (int n = 0; n < NV; ++n) o[n] *= down;
-                }
                 // fp16 tokens: weights in two parts, as their rounding would show beside that of the results (relative error of four
                 // masked rows of 100k keys 3.3e-4 in the place of 2.1e-4, which the results' rounding alone makes; bf16's is eight times
                 // that).  It costs 2 us of 38 there.
                 constexpr int NP = DT == SPARGE_F16 ? 4 : 2;
                 v8h pf[NP];
-                softmax<NV>(s, qs * (ka * (1.0f / 127.0f)), vs, block * PAGE + PAGE - 1 > all_limit, my_limit - block * PAGE, m, l, o, pf);
+                softmax<NV>(s, qs * (ka * (1.0f / 127.0f)), log2_of(va), block * PAGE + PAGE - 1 > all_limit, my_limit - block * PAGE, m, mo, l, o, pf);
                 if (bad && my_limit + 4 * (lane >> 4) >= block * PAGE) l = nan_f();
 #pragma unroll
                 for (int n = 0; n < NV; ++n) {
@@ -550,11 +552,11 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
         }
         l = sum_groups(l);
         if (mine_valid) {
-            const float inv = inverse(l);
+            const Mean mean(l, m, mo);
             if (it.b0 == 0 && it.b1 == it.blocks) {
-                store_whole<NV, DT>(o, inv, vs.ref, O + my_token * a.o_sn + my_head * a.o_sh + 4 * (lane >> 4));
+                store_whole<NV, DT>(o, mean, O + my_token * a.o_sn + my_head * a.o_sh + 4 * (lane >> 4));
             } else {
-                store_part<NV>(o, m, l, inv, vs.ref, ws, static_cast<long long>(2 * part + (it.b0 > 0 ? 0 : 1)) * NARROW_ROWS + (lane & 15));
+                store_part<NV>(o, mean, m, l, ws, static_cast<long long>(2 * part + (it.b0 > 0 ? 0 : 1)) * NARROW_ROWS + (lane & 15));
             }
         }
         it = nx;
@@ -734,13 +736,12 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
         }
         v8h qf[KS];
         const float qs = a.scale_log2 * (1.0f / 127.0f) * convert_q32<D, DT>(q_raw, qf);
-        float m = FAR, l = 0.f;
+        float m = FAR, mo = FAR, l = 0.f;
         v16f o[NC];
 #pragma unroll
         for (int n = 0; n < NC; ++n)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[n][e] = 0.f;
-        VScale vs;
         if (more) {
             convert(0);
             n_more = blocks.next(c, kh, n_block, page, n_at);
@@ -790,25 +791,22 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
 #pragma unroll
                 for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
             top = fmaxf(top, other<32>(top)) * cq;
-            float down = vs.take(va);
-            const float to = fmaxf(m, top);
-            if (__any(top > m + SLACK) || down != 1.0f) {
-                const bool moves = __any(top > m + SLACK);
-                const float dm = moves ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
-                if (moves) m = to;
-                l *= dm;
-                down *= dm;
+            const float v_log2 = log2_of(va);
+            if (__any(top > m + SLACK || top + v_log2 > mo + SLACK)) {
+                const float to = fmaxf(m, top), o_to = fmaxf(mo, top + v_log2), down = __builtin_amdgcn_exp2f(mo - o_to);
+                l *= __builtin_amdgcn_exp2f(m - to);
+                m = to, mo = o_to;
 #pragma unroll
                 for (int n = 0; n < NC; ++n) o[n] *= down;
             }
-            const float from = vs.f_log2 - m;
+            const float add = weight_log2(v_log2, mo, top);
             float sum = 0.f;
             v8h pf[4], rest[4], v[4];
             auto weights = [&](int u, int e) {   // two of the eight of step u
 #pragma unroll
                 for (int k = e; k < e + 2; ++k) {
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + k], cq, from));
-                    sum += w;   // before its rounding: w carries V's factor, which may be small
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + k], cq, add));
+                    sum += w;   // before its rounding: w carries V's scale, which may be small
                     pf[u][k] = static_cast<_Float16>(w);
                     if constexpr (TWO) rest[u][k] = static_cast<_Float16>(w - static_cast<float>(pf[u][k]));
                 }
@@ -832,7 +830,7 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            l += sum * vs.f_inv;
+            l += sum * weight_back(add, m);
         };
         for (int buf = 0; more; buf ^= 1) {
             // the next block's bytes into the other buffer (nobody reads it; behind the last block whatever is there), the one
@@ -867,7 +865,7 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
 
         l += other<32>(l);
         if (valid) {
-            const float inv = inverse(l);
+            const Mean mean(l, m, mo);
             uint16_t* out = O + token * a.o_sn + hd * a.o_sh + 4 * half;
             const long long row_at = static_cast<long long>(2 * part + (x0 > 0 ? 0 : 1)) * WIDE_ROWS + row;
 #pragma unroll
@@ -876,7 +874,7 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
                 for (int e = 0; e < 4; ++e) {   // channels 32 n + 8 e + 4 half + 0..3
                     v4f y;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) y[k] = o[n][4 * e + k] * inv * vs.ref;
+                    for (int k = 0; k < 4; ++k) y[k] = mean(o[n][4 * e + k]);
                     if (whole) {
                         uint16_t h[4];
 #pragma unroll
