@@ -10,13 +10,14 @@
 // in blocks that it gives no weight.
 //
 // The query rows of one row of the cache are its new tokens times the G heads that share a kv head.  Two kernels:
-//   rows of at most 16 query rows (decoding): the work is reading pages.  A wave takes blocks by itself, operands come
+//   rows of at most 16 query rows (decoding), and of more where all is little: the work is reading pages.  A wave takes blocks by itself, operands come
 //   from memory into registers, 1 KB of consecutive bytes a load, without LDS and without barriers.
-//   rows of more: the work is products.  Four waves take 32 query rows each and share the blocks, which they convert to
+//   others: the work is products.  Four waves take 32 query rows each and share the blocks, which they convert to
 //   fp16 into LDS once, a quarter each.
 // In both, items (a kv head's tile of query rows) lie one behind the other on a line, each as long as the keys it sees; the
 // line is cut into equal parts, one per wave or workgroup.  A long item is split over several parts, whose results a
-// further launch joins in a fixed order; short ones share a part.
+// further launch joins in a fixed order; short ones share a part.  The host knows the step's tokens but not which rows have them: where
+// rows of both kinds are possible, one launch's workgroups take their parts of the first line, then, if there are any, of the second.
 #include "cache.hpp"
 
 namespace sparge {
@@ -36,6 +37,10 @@ constexpr float W_LEAST = 60.0f;       // log2: a block whose largest weight wou
 
 constexpr int NARROW_ROWS = 16, NARROW_WGS = 512, NARROW_LOG2 = 11;   // two workgroups per compute unit, a part per wave
 constexpr int WIDE_ROWS = 128, WIDE_WGS = 512, WIDE_LOG2 = 9;         // a part per workgroup
+// Rows of several tiles are the narrow kernel's too where the whole line is at most 5 blocks a wave: the wide kernel's workgroups would
+// have few blocks each, one after the other (4 rows of 9000 keys, 16 heads a kv head, 8 tokens: 30 us in the place of 46; of 4 heads and
+// 8 tokens: 33.0, 36.9; 8.8 blocks a wave, 4 heads and 16 tokens: 53.7, 46.4).
+constexpr u64 NARROW_BLOCKS = 5;
 static_assert(4 * NARROW_WGS == 1 << NARROW_LOG2 && WIDE_WGS == 1 << WIDE_LOG2, "the line is cut into up to 2^LOG2 parts");
 
 template <int X>
@@ -56,6 +61,11 @@ __device__ __forceinline__ float max_groups(float v) {
 __device__ __forceinline__ float sum_groups(float v) {
     v += other<16>(v);
     return v + other<32>(v);
+}
+// What the narrow and the wide half of a kernel make of a value is not kept in registers from the one to the other.
+__device__ __forceinline__ int opaque(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ u64 uniform(u64 v) {
@@ -88,20 +98,25 @@ __host__ __device__ inline Cut cut_of(int G, int rows) {
     return {G, rows, (G + rows - 1) / rows, 1};
 }
 
-// Which rows a launch takes: all, those of at most 16 query rows, or the others.
-enum Rows { ALL_ROWS, FEW_ROWS, MANY_ROWS };
+// Which rows a line holds: those of more than `above` and at most `upto` query rows of a kv head.
+struct Rows {
+    long long above, upto;
+
+    __device__ __forceinline__ bool hold(int n, int G) const { return static_cast<long long>(n) * G > above && static_cast<long long>(n) * G <= upto; }
+};
+constexpr Rows ALL_ROWS = {0, 1ll << 62};
 
 struct RowInfo {
-    int first, n, len, p0;     // new tokens [first, first + n) (0: not this launch's), keys, keys before the first new token
+    int first, n, len, p0;     // new tokens [first, first + n) (0: not this line's), keys, keys before the first new token
     int tiles;                 // tiles of TT tokens
 };
-__device__ __forceinline__ RowInfo row_info(const sparge_cache& c, const CacheAttn& a, const Cut& t, Rows which, int r) {
+__device__ __forceinline__ RowInfo row_info(const sparge_cache& c, const CacheAttn& a, const Cut& t, const Rows& which, int r) {
     RowInfo x;
     x.first = max(0, min(a.cu[r], a.n_slots));
     x.n = max(0, min(a.cu[r + 1], a.n_slots) - x.first);
     x.len = max(0, min(c.length[r], static_cast<int>(min(static_cast<long long>(c.max_blocks) * PAGE, 0x7FFFFFC0ll))));
     x.p0 = max(0, x.len - x.n);
-    if (which != ALL_ROWS && (static_cast<long long>(x.n) * t.G <= NARROW_ROWS) != (which == FEW_ROWS)) x.n = 0;
+    if (!which.hold(x.n, t.G)) x.n = 0;
     x.tiles = (x.n + t.TT - 1) / t.TT;
     return x;
 }
@@ -116,18 +131,26 @@ struct Joint {                          // workspace
     float* o;                           // [2 parts][rows of a tile][d] mean of the values over the part's keys
 };
 
-// exclusive prefix of v over the 256 threads and the total; lds: 4 values
-__device__ __forceinline__ u64 prefix(u64 v, u64* lds, u64& total) {
+// exclusive prefixes of v over the 256 threads and the totals; lds: 4 per value
+template <int N>
+__device__ __forceinline__ void prefix(u64 (&v)[N], u64 (*lds)[4], u64 (&total)[N]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    u64 upto = scan_lanes(static_cast<long long>(v));
-    if (lane == 63) lds[wave] = upto;
-    __syncthreads();
-    total = 0;
-    for (int w = 0; w < 4; ++w) {
-        if (w < wave) upto += lds[w];
-        total += lds[w];
+    u64 upto[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        upto[k] = scan_lanes(static_cast<long long>(v[k]));
+        if (lane == 63) lds[k][wave] = upto[k];
     }
-    return upto - v;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        total[k] = 0;
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) upto[k] += lds[k][w];
+            total[k] += lds[k][w];
+        }
+        v[k] = upto[k] - v[k];
+    }
 }
 
 // a / b, both below 2^52.  (Kernels that run for a few microseconds wait for their own instructions: the 64-bit division that the
@@ -360,34 +383,65 @@ __device__ __forceinline__ void store_part(const v4f (&o)[NV], const Mean& mean,
 // in the place of 100.)  A lone row of 500 keys takes 7.6 us, a chain of latencies: the rows' sums, the table, the
 // queries, the page.
 struct NarrowShared {
-    u64 sums[4], before[256];           // per thread: places on the line before its rows, the first of these
+    u64 sums[2][4], before[256];        // per thread: places on the line before its rows, the first of these
     RowInfo info[256];
 };
-template <int D, int DT>
-__device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a, Rows which, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
-                                       const Joint& ws, int bid, NarrowShared& sh) {
-    constexpr int NK = 4 * D / 64, NV = D / 16, KS = D / 32;
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const Cut cut = cut_of(a.H / c.H_kv, NARROW_ROWS);
-    const int heads = c.H_kv * cut.parts;
-
-    // ---- this wave's part of the line, in blocks.  (All tiles of a row count with all its blocks: they are few here.)
-    const int per = (c.R + 255) / 256;
-    auto blocks_in = [&](const RowInfo& x) { return x.n ? (x.len + PAGE - 1) / PAGE : 0; };
-    auto length_of = [&](const RowInfo& x) { return static_cast<u64>(x.tiles) * heads * blocks_in(x); };
+// The line of blocks.  (All tiles of a row count with all its blocks: they are few here.)
+struct NarrowLine {
+    Cut cut;
+    int heads, per;                     // pieces of heads; rows per thread
     Line line;
-    const int r0 = tid * per, r1 = min(r0 + per, c.R);
+    Rows which;                         // its rows
+    bool others;                        // whether there are others
+
+    __device__ __forceinline__ int blocks_in(const RowInfo& x) const { return x.n ? (x.len + PAGE - 1) / PAGE : 0; }
+    __device__ __forceinline__ u64 length_of(const RowInfo& x) const { return static_cast<u64>(x.tiles) * heads * blocks_in(x); }
+};
+// MIXED: there may be rows of more than one tile.
+template <bool MIXED>
+__device__ __forceinline__ NarrowLine narrow_line(const sparge_cache& c, const CacheAttn& a, NarrowShared& sh) {
+    NarrowLine x;
+    x.cut = cut_of(a.H / c.H_kv, NARROW_ROWS);
+    x.heads = c.H_kv * x.cut.parts, x.per = (c.R + 255) / 256, x.which = ALL_ROWS, x.others = false;
+    const int tid = threadIdx.x, r0 = tid * x.per, r1 = min(r0 + x.per, c.R);
+    constexpr int N = MIXED ? 2 : 1;    // rows of one tile; of several
+    u64 mine[N] = {}, total[N];
+    auto add = [&](const RowInfo& row) {
+        const u64 length = x.length_of(row);
+        const bool one = !MIXED || row.n <= x.cut.TT;
+        mine[0] += one ? length : 0;
+        if constexpr (MIXED) mine[1] += one ? 0 : length;
+    };
     RowInfo row0 = {0, 0, 0, 0, 0};
-    if (r0 < r1) row0 = row_info(c, a, cut, which, r0);
-    u64 mine = length_of(row0);
+    if (r0 < r1) row0 = row_info(c, a, x.cut, ALL_ROWS, r0);
+    add(row0);
 #pragma unroll 1
-    for (int r = r0 + 1; r < r1; ++r) mine += length_of(row_info(c, a, cut, which, r));
-    const u64 before = prefix(mine, sh.sums, line.total);
-    line.total = uniform(line.total);
-    line.log2 = line.total >> NARROW_LOG2 ? NARROW_LOG2 : line.total ? 63 - __builtin_clzll(line.total) : 0;
-    const int parts = line.total ? 1 << line.log2 : 0, part = bid * 4 + wave;
-    sh.before[tid] = before, sh.info[tid] = row0;
+    for (int r = r0 + 1; r < r1; ++r) add(row_info(c, a, x.cut, ALL_ROWS, r));
+    prefix(mine, sh.sums, total);
+    x.line.total = uniform(total[0]);
+    if constexpr (MIXED) {
+        const u64 more = uniform(total[1]);
+        x.others = more && x.line.total + more > NARROW_BLOCKS << NARROW_LOG2;
+        if (x.others) {
+            x.which.upto = NARROW_ROWS;
+            if (!x.which.hold(row0.n, x.cut.G)) row0.n = row0.tiles = 0;
+        } else {
+            x.line.total += more, mine[0] += mine[1];
+        }
+    }
+    x.line.log2 = x.line.total >> NARROW_LOG2 ? NARROW_LOG2 : x.line.total ? 63 - __builtin_clzll(x.line.total) : 0;
+    sh.before[tid] = mine[0], sh.info[tid] = row0;
     __syncthreads();
+    return x;
+}
+template <int D, int DT>
+__device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a, const NarrowLine& rows, const uint16_t* __restrict__ Q,
+                                       uint16_t* __restrict__ O, const Joint& ws, int bid, const NarrowShared& sh) {
+    constexpr int NK = 4 * D / 64, NV = D / 16, KS = D / 32;
+    const int tid = opaque(threadIdx.x), lane = tid & 63, wave = uniform(tid >> 6), heads = rows.heads;
+    const Cut& cut = rows.cut;
+    const Line& line = rows.line;
+    const int parts = line.total ? 1 << line.log2 : 0, part = bid * 4 + wave;
     if (part >= parts) {
         if (lane == 0) ws.desc[part] = NO_JOIN;
         return;
@@ -398,15 +452,15 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
     int t = -1;
 #pragma unroll
     for (int e = 0; e < 4; ++e) t += __builtin_popcountll(__ballot(sh.before[4 * lane + e] <= lo));
-    int r = t * per;
+    int r = t * rows.per;
     u64 rem = lo - uniform(sh.before[t]);
     RowInfo info = uniform(sh.info[t]);
 #pragma unroll 1
-    while (rem >= length_of(info) && r < c.R - 1) {
-        rem -= length_of(info);
-        info = uniform(row_info(c, a, cut, which, ++r));
+    while (rem >= rows.length_of(info) && r < c.R - 1) {
+        rem -= rows.length_of(info);
+        info = uniform(row_info(c, a, cut, rows.which, ++r));
     }
-    int row_blocks = blocks_in(info);
+    int row_blocks = rows.blocks_in(info);
     u64 left = line.begin(part + 1) - lo;                     // blocks that this wave still has to take
     const u64 in_row = row_blocks ? quotient(rem, row_blocks) : 0;
     int b_next = static_cast<int>(rem - in_row * row_blocks);
@@ -426,8 +480,8 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
                 head = 0;
                 do {
                     if (++r >= c.R) return false;
-                    info = uniform(row_info(c, a, cut, which, r));
-                    row_blocks = blocks_in(info);
+                    info = uniform(row_info(c, a, cut, rows.which, r));
+                    row_blocks = rows.blocks_in(info);
                 } while (row_blocks == 0);
             }
         }
@@ -603,19 +657,19 @@ __device__ __forceinline__ float convert_q32(const uint4 (&raw)[D / 16], v8h (&q
 // 4 (lane / 32) + 0..3 and those + 8; V's operands are laid out for that order.
 template <int D>
 struct WideShared {
-    u64 sums[4], rem;
+    u64 sums[1][4], rem;
     int row;
     RowInfo info;
     __align__(16) v8h k[2][2 * D / 16 * 64], v[2][D / 32 * 4 * 64];
 };
 // TWO: weights in two parts, as in the narrow kernel.
 template <int D, int DT, bool TWO>
-__device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, Rows which, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
+__device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, const Rows& which, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
                                      const Joint& ws, int bid, WideShared<D>& sh) {
     constexpr int KS = D / 16, NC = D / 32, RAW = D / 64;   // steps of K Q^T, channel tiles, 16-byte pieces of K (of V) per thread
     auto& lds_k = sh.k;
     auto& lds_v = sh.v;
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
+    const int tid = opaque(threadIdx.x), lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
     const Cut cut = cut_of(a.H / c.H_kv, WIDE_ROWS);
     const int heads = c.H_kv * cut.parts;
 
@@ -629,8 +683,10 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
     u64 mine = length_of(row0) * heads;
 #pragma unroll 1
     for (int r = r0 + 1; r < r1; ++r) mine += length_of(row_info(c, a, cut, which, r)) * heads;
-    const u64 before = prefix(mine, sh.sums, line.total);
-    line.total = uniform(line.total);
+    u64 upto[1] = {mine}, total[1];
+    prefix(upto, sh.sums, total);
+    const u64 before = upto[0];
+    line.total = uniform(total[0]);
     // parts of at least two blocks; neighbours on the line, which share pages, are neighbours on an XCD
     const u64 wanted = line.total / (2 * PAGE);
     line.log2 = wanted >> WIDE_LOG2 ? WIDE_LOG2 : wanted ? 63 - __builtin_clzll(wanted) : 0;
@@ -903,11 +959,12 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
     if (tid == 0) ws.desc[bid] = join;
 }
 
-// ---- the launches: rows of the one kind, of the other, or both side by side
+// ---- the launches: rows of the one kind, of the other, or of both
 template <int D, int DT>
 __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache c, CacheAttn a, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O, Joint ws) {
     __shared__ NarrowShared sh;
-    narrow<D, DT>(c, a, ALL_ROWS, Q, O, ws, blockIdx.x, sh);
+    const NarrowLine rows = narrow_line<false>(c, a, sh);
+    narrow<D, DT>(c, a, rows, Q, O, ws, blockIdx.x, sh);
 }
 template <int D, int DT, bool TWO>
 __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c, CacheAttn a, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O, Joint ws) {
@@ -917,13 +974,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c,
 template <int D, int DT, bool TWO>
 __global__ __launch_bounds__(256, 2) void cache_attn_both_kernel(sparge_cache c, CacheAttn a, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
                                                                  Joint ws_wide, Joint ws_narrow) {
-    __shared__ union Shared {
-        __device__ Shared() {}
-        WideShared<D> wide;
-        NarrowShared narrow;
-    } sh;
-    if (blockIdx.x < WIDE_WGS) wide<D, DT, TWO>(c, a, MANY_ROWS, Q, O, ws_wide, blockIdx.x, sh.wide);
-    else narrow<D, DT>(c, a, FEW_ROWS, Q, O, ws_narrow, blockIdx.x - WIDE_WGS, sh.narrow);
+    __shared__ NarrowShared sh;
+    __shared__ WideShared<D> sh_wide;
+    static_assert(WIDE_WGS == NARROW_WGS, "a workgroup has a part of either line");
+    // the wide part first: where it has ended, the narrow one's four waves end each by itself
+    const NarrowLine rows = narrow_line<true>(c, a, sh);
+    if (rows.others) wide<D, DT, TWO>(c, a, Rows{NARROW_ROWS, ALL_ROWS.upto}, Q, O, ws_wide, blockIdx.x, sh_wide);
+    else if (threadIdx.x == 0) ws_wide.desc[blockIdx.x] = NO_JOIN;
+    narrow<D, DT>(c, a, rows, Q, O, ws_narrow, blockIdx.x, sh);
 }
 
 // ---- join ----------------------------------------------------------------------------------------------------------
@@ -999,12 +1057,12 @@ __device__ __forceinline__ void join(const sparge_cache& c, const CacheAttn& a, 
     else if (d.n_parts <= 64) join_item<D, DT, ROWS, 8>(d, me, workers, Gp, a, O, ws);
     else join_item<D, DT, ROWS, 32>(d, me, workers, Gp, a, O, ws);
 }
-// the first n_wide workgroups take the wide kernel's parts, the others the narrow one's
+// the first n_narrow workgroups take the narrow kernel's parts, the others the wide one's
 template <int D, int DT>
-__global__ __launch_bounds__(256) void cache_join_kernel(sparge_cache c, CacheAttn a, int n_wide, uint16_t* __restrict__ O, Joint ws_wide, Joint ws_narrow) {
+__global__ __launch_bounds__(256) void cache_join_kernel(sparge_cache c, CacheAttn a, int n_narrow, uint16_t* __restrict__ O, Joint ws_wide, Joint ws_narrow) {
     const int bid = blockIdx.x;
-    if (bid < n_wide) join<D, DT, WIDE_ROWS, 4>(c, a, O, ws_wide, bid);
-    else join<D, DT, NARROW_ROWS, 1>(c, a, O, ws_narrow, bid - n_wide);
+    if (bid < n_narrow) join<D, DT, NARROW_ROWS, 1>(c, a, O, ws_narrow, bid);
+    else join<D, DT, WIDE_ROWS, 4>(c, a, O, ws_wide, bid - n_narrow);
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -1032,7 +1090,7 @@ void launch(const sparge_cache& c, const CacheAttn& a, bool narrow, bool wide, c
     uint16_t* O = static_cast<uint16_t*>(Op);
     auto many = [&](auto two) {
         constexpr bool TWO = decltype(two)::value;
-        if (narrow) hipLaunchKernelGGL((cache_attn_both_kernel<D, DT, TWO>), dim3(WIDE_WGS + NARROW_WGS), dim3(256), 0, st, c, a, Q, O, j[0], j[1]);
+        if (narrow) hipLaunchKernelGGL((cache_attn_both_kernel<D, DT, TWO>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, Q, O, j[0], j[1]);
         else hipLaunchKernelGGL((cache_attn_wide_kernel<D, DT, TWO>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, Q, O, j[0]);
     };
     // The second part of fp16's weights, where reading pages counts for more than products: up to 64 query rows a row of the cache on
@@ -1043,7 +1101,7 @@ void launch(const sparge_cache& c, const CacheAttn& a, bool narrow, bool wide, c
     else if (wide) many(std::false_type{});
     else hipLaunchKernelGGL((cache_attn_narrow_kernel<D, DT>), dim3(NARROW_WGS), dim3(256), 0, st, c, a, Q, O, j[1]);
     const int n_wide = wide ? WIDE_WGS : 0, n_narrow = narrow ? NARROW_WGS : 0;
-    hipLaunchKernelGGL((cache_join_kernel<D, DT>), dim3(n_wide + n_narrow), dim3(256), 0, st, c, a, n_wide, O, j[0], j[1]);
+    hipLaunchKernelGGL((cache_join_kernel<D, DT>), dim3(n_wide + n_narrow), dim3(256), 0, st, c, a, n_narrow, O, j[0], j[1]);
 }
 
 }  // namespace
@@ -1057,14 +1115,13 @@ hipError_t launch_cache_attn(const sparge_cache& c, const CacheAttn& a, const vo
     for (int k = 0; k < 2; ++k)
         j[k] = {reinterpret_cast<JoinDesc*>(p + x.desc[k]), reinterpret_cast<float*>(p + x.ml[k]), reinterpret_cast<float*>(p + x.o[k])};
     // How many tokens each row adds is not known here.  Groups beyond a wave's 16 rows are the wide kernel's (16 rows, 8 queries a head: narrow
-    // 26 us, wide 36; 16 queries: 30 and 38).  Up to 16 tokens more than rows (one each, and what pads a batch), or up to half a
-    // wave's rows on average, are taken for decoding: the narrow kernel alone, which gives the right result for longer rows, too
-    // (64 rows of 300 to 9000 keys, 4 queries a head: 1 token 72 us, wide 113, both 74; 2 tokens 78, 111, 80; 8 tokens 129, 123, 124).
-    // More of them in a single row are the wide kernel's (9000 keys, 4 queries a head: 2 tokens narrow 17.8 us, wide 18.1; 4 tokens
-    // 22.3 and 18.6; 8 tokens 27.2 and 18.9); else both run side by side, each on its rows (8 rows of 1 to 600 tokens: both 140 us,
-    // wide 142, narrow 268).
-    const long long G = a.H / c.H_kv;
-    const bool few = a.n_slots <= (c.R > 1 ? c.R + 16 : 1) || a.n_slots * G <= NARROW_ROWS / 2 * c.R;
+    // 26 us, wide 36; 16 queries: 30 and 38).  The narrow kernel alone runs where no row can have more than a tile; a single row's
+    // tokens are the wide kernel's from half a tile on (9000 keys, 4 queries a head: 2 tokens narrow 17.8 us, wide 18.1; 4 tokens 22.3
+    // and 18.6; 8 tokens 27.2 and 18.9).  Else one kernel holds both, which costs a step of single tokens 0.1 to 0.9 us, and shares
+    // the rows out on the device (255 rows of one token beside one of 1500 over 30000 keys, 1 query a head: 554 us, the narrow kernel
+    // alone 1124; one row of 500 tokens over 9000 keys among 511 idle ones: 144 and 276).
+    const long long G = a.H / c.H_kv, most = a.n_slots * G;
+    const bool few = c.R > 1 ? most <= NARROW_ROWS : a.n_slots == 1 || most <= NARROW_ROWS / 2;
     const bool narrow = G <= NARROW_ROWS && (few || c.R > 1), wide = G > NARROW_ROWS || !few;
 #define RUN(D, DT) launch<D, DT>(c, a, narrow, wide, Q, O, j, st)
     if (c.d == 64) {

@@ -1,0 +1,69 @@
+"""Steps whose rows differ: which rows a workgroup takes together, and how, is decided on the device from the rows' tokens and keys.  Rows of
+several tiles of 16 query rows in little work and in much, one row among idle ones, pieces beside decoding rows."""
+import numpy as np
+import pytest
+
+from cache_cases import Model
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sp():
+    import paper_2502_18137_amd as sp
+    return sp
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("G,new", [(16, [18, 0]), (5, [4, 1]), (4, [5, 30]), (3, [40, 0, 2, 6]), (1, [130, 1]), (1, [17, 17, 16]), (7, [33, 1, 2])])
+def test_rows_of_several_tiles_in_little_work(sp, G, new, dtype, causal):
+    """at most a few blocks a wave: waves take them tile by tile, the last one of fewer tokens"""
+    m = Model(sp, len(new), 2, 128 if G < 5 else 64, 80, 30, dtype=dtype, seed=90 + G)
+    m.step(([300, 70, 0, 64] * 2)[:len(new)])
+    plan = m.step(new, pad=2)
+    m.check_attn(plan, 2 * G, causal=causal, pad=2)
+    mask = (m.rng.random((len(new), 2, 30)) < 0.5).astype(np.uint8)
+    m.check_attn(plan, 2 * G, causal=causal, mask=mask, pad=2)
+
+
+@pytest.mark.parametrize("new", [159, 160, 161])
+def test_the_most_that_counts_as_little(sp, new):
+    """tiles of one token, 64 blocks of keys each: up to 10240 blocks are waves' work, more are workgroups'"""
+    m = Model(sp, 2, 1, 64, 140, 70, dtype="bf16", seed=new)
+    m.step([4096 - new, 0])
+    m.check_attn(m.step([new, 0]), 16)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("G,piece,others", [(4, 300, 0), (4, 300, 1), (1, 700, 0), (1, 700, 1), (2, 300, 2), (16, 40, 1)])
+def test_one_row_among_many(sp, G, piece, others, dtype):
+    """one row's piece of a prompt, the other 299 idle, or adding one token, or two; rows in any place"""
+    m = Model(sp, 300, 2, 64, 900, 100, dtype=dtype, seed=100 + G + others)
+    long = 5000 if G < 16 else 6000
+    held = [int(n) for n in m.rng.integers(0, 100, 300)]
+    held[131] = long
+    m.step(held)
+    new = [others] * 300
+    new[131], new[7], new[299] = piece, 0, 3
+    m.check_attn(m.step(new, pad=1), 2 * G, pad=1)
+
+
+def test_the_same_step_again_and_again(sp):
+    """the same bits on every call, whatever an earlier call left in the workspace"""
+    import torch
+    m = Model(sp, 40, 2, 128, 300, 60, dtype="bf16", seed=110)
+    m.step([3000] + [50] * 39)
+    mixed = m.step([200] + [1] * 39)
+    q = m.gpu(m.queries(8))
+    ws = torch.full((sp.sparge_cache_attn_workspace_bytes(m.cache, 8),), 255, dtype=torch.uint8, device="cuda")
+    first = sp.sparge_cache_attn(m.cache, q, mixed, ws=ws).clone()
+    m.check_attn(mixed, 8, q=q.double().cpu().numpy())
+    small = m.step([3, 9] + [0] * 38)
+    few = sp.sparge_cache_attn(m.cache, q[:12], small, ws=ws).clone()
+    m.check_attn(small, 8, q=q[:12].double().cpu().numpy())
+    for _ in range(2):
+        assert torch.equal(sp.sparge_cache_attn(m.cache, q[:12], small, ws=ws), few)
+    ws.fill_(0x7F)
+    assert torch.equal(sp.sparge_cache_attn(m.cache, q[:12], small, ws=ws), few)
+    assert bool(torch.isfinite(first.float()).all())
