@@ -365,8 +365,8 @@ int sparge_cache_read(const sparge_cache* cache, const int32_t* slots, const int
  * O_i = sum_j softmax_j(sm_scale q_i . k_j) v_j over the keys that it sees, 0 if there are none; rows of O behind
  * cu[R] stay as they were.  sm_scale <= 0 selects 1/sqrt(d).
  * Products are 16-bit with fp32 sums; the codes enter them exactly (integers up to 127 in fp16), Q as it is (bf16 times a
- * power of two per row, in fp16), the weights times V's scale rounded to fp16 (fp16 tokens, up to 64 query rows of a kv head
- * per row on average: in two parts, to 22 bits) beside the query's own largest weight times scale, of which they keep what is 2^-34 or
+ * power of two per row, in fp16), the weights times V's scale rounded to fp16 (fp16 tokens, rows of up to 64 query rows of a kv
+ * head: in two parts, to 22 bits) beside the query's own largest weight times scale, of which they keep what is 2^-34 or
  * more; weights below 2^-126 of a query's largest may count as 0.  The result does not depend on timing.
  * O must not overlap Q.  The workspace (256-byte aligned) carries nothing between calls; calls that may overlap need one each.
  */

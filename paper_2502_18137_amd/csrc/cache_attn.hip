@@ -662,8 +662,13 @@ struct WideShared {
     RowInfo info;
     __align__(16) v8h k[2][2 * D / 16 * 64], v[2][D / 32 * 4 * 64];
 };
-// TWO: weights in two parts, as in the narrow kernel.
-template <int D, int DT, bool TWO>
+// fp16: the weights of rows of up to TWO_ROWS query rows are in two parts, as in the narrow kernel: there reading pages counts for more than
+// products (32 rows of one token, 32 heads a kv head: 47.1 us in the place of 45; prompts of 1000 tokens would take 840 us in the
+// place of 650, and theirs are many rows: 1.25 times the error of the results' own rounding).  By the row, so that its bits and its
+// cost do not depend on the other rows; the branches cost the prompts 1 %.  (The second part behind all products of the first, which read
+// V's operands once more: 50.7 us.  Two copies of the loop: registers spill, twice the time.)
+constexpr int TWO_ROWS = WIDE_ROWS / 2;
+template <int D, int DT>
 __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, const Rows& which, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
                                      const Joint& ws, int bid, WideShared<D>& sh) {
     constexpr int KS = D / 16, NC = D / 32, RAW = D / 64;   // steps of K Q^T, channel tiles, 16-byte pieces of K (of V) per thread
@@ -830,6 +835,7 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
             }
             static_assert(CHUNKS == KS, "a chunk for every other product");
         };
+        const bool two = DT == SPARGE_F16 && static_cast<long long>(x.n) * cut.G <= TWO_ROWS;
         auto weigh = [&](bool masked, int buf) {
             float cq = qs * ka;
             if (cq == 0.f) cq = 1e-37f;   // a block of zeros: -inf stays what it is and becomes a weight of 0
@@ -857,14 +863,14 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
             }
             const float add = weight_log2(v_log2, mo, top);
             float sum = 0.f;
-            v8h pf[4], rest[4], v[4];
+            v8h pf[4], v[4], rest;
             auto weights = [&](int u, int e) {   // two of the eight of step u
 #pragma unroll
                 for (int k = e; k < e + 2; ++k) {
                     const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u >> 1][8 * (u & 1) + k], cq, add));
+                    s[u >> 1][8 * (u & 1) + k] = w;
                     sum += w;   // before its rounding: w carries V's scale, which may be small
                     pf[u][k] = static_cast<_Float16>(w);
-                    if constexpr (TWO) rest[u][k] = static_cast<_Float16>(w - static_cast<float>(pf[u][k]));
                 }
                 asm volatile("" : "+v"(sum));   // here, not all of them behind the last product
             };
@@ -878,7 +884,13 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
             for (int x = 0; x < 4 * NC; ++x) {
                 const int u = x / NC, n = x % NC;
                 o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x & 3], pf[u], o[n], 0, 0, 0);
-                if constexpr (TWO) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x & 3], rest[u], o[n], 0, 0, 0);
+                if (two) {   // what the weights' rounding left
+                    if (n == 0) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) rest[k] = static_cast<_Float16>(s[u >> 1][8 * (u & 1) + k] - static_cast<float>(pf[u][k]));
+                    }
+                    o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x & 3], rest, o[n], 0, 0, 0);
+                }
                 if (x + 4 < 4 * NC) v[x & 3] = operand(x + 4);
                 if (u < 3) {
 #pragma unroll
@@ -966,12 +978,12 @@ __global__ __launch_bounds__(256, 2) void cache_attn_narrow_kernel(sparge_cache 
     const NarrowLine rows = narrow_line<false>(c, a, sh);
     narrow<D, DT>(c, a, rows, Q, O, ws, blockIdx.x, sh);
 }
-template <int D, int DT, bool TWO>
+template <int D, int DT>
 __global__ __launch_bounds__(256, 2) void cache_attn_wide_kernel(sparge_cache c, CacheAttn a, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O, Joint ws) {
     __shared__ WideShared<D> sh;
-    wide<D, DT, TWO>(c, a, ALL_ROWS, Q, O, ws, blockIdx.x, sh);
+    wide<D, DT>(c, a, ALL_ROWS, Q, O, ws, blockIdx.x, sh);
 }
-template <int D, int DT, bool TWO>
+template <int D, int DT>
 __global__ __launch_bounds__(256, 2) void cache_attn_both_kernel(sparge_cache c, CacheAttn a, const uint16_t* __restrict__ Q, uint16_t* __restrict__ O,
                                                                  Joint ws_wide, Joint ws_narrow) {
     __shared__ NarrowShared sh;
@@ -979,7 +991,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_both_kernel(sparge_cache c,
     static_assert(WIDE_WGS == NARROW_WGS, "a workgroup has a part of either line");
     // the wide part first: where it has ended, the narrow one's four waves end each by itself
     const NarrowLine rows = narrow_line<true>(c, a, sh);
-    if (rows.others) wide<D, DT, TWO>(c, a, Rows{NARROW_ROWS, ALL_ROWS.upto}, Q, O, ws_wide, blockIdx.x, sh_wide);
+    if (rows.others) wide<D, DT>(c, a, Rows{NARROW_ROWS, ALL_ROWS.upto}, Q, O, ws_wide, blockIdx.x, sh_wide);
     else if (threadIdx.x == 0) ws_wide.desc[blockIdx.x] = NO_JOIN;
     narrow<D, DT>(c, a, rows, Q, O, ws_narrow, blockIdx.x, sh);
 }
@@ -1088,17 +1100,8 @@ template <int D, int DT>
 void launch(const sparge_cache& c, const CacheAttn& a, bool narrow, bool wide, const void* Qp, void* Op, const Joint (&j)[2], hipStream_t st) {
     const uint16_t* Q = static_cast<const uint16_t*>(Qp);
     uint16_t* O = static_cast<uint16_t*>(Op);
-    auto many = [&](auto two) {
-        constexpr bool TWO = decltype(two)::value;
-        if (narrow) hipLaunchKernelGGL((cache_attn_both_kernel<D, DT, TWO>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, Q, O, j[0], j[1]);
-        else hipLaunchKernelGGL((cache_attn_wide_kernel<D, DT, TWO>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, Q, O, j[0]);
-    };
-    // The second part of fp16's weights, where reading pages counts for more than products: up to 64 query rows a row of the cache on
-    // average (32 rows of one token and 32 heads: 29.9 us in the place of 28.8; prompts of 1000 tokens would take 840 us in the
-    // place of 652, and theirs are many rows: 1.25 times the error of the results' own rounding).
-    const bool two = DT == SPARGE_F16 && static_cast<long long>(a.n_slots) * (a.H / c.H_kv) <= WIDE_ROWS / 2 * c.R;
-    if (wide && two) many(std::bool_constant<DT == SPARGE_F16>{});
-    else if (wide) many(std::false_type{});
+    if (narrow && wide) hipLaunchKernelGGL((cache_attn_both_kernel<D, DT>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, Q, O, j[0], j[1]);
+    else if (wide) hipLaunchKernelGGL((cache_attn_wide_kernel<D, DT>), dim3(WIDE_WGS), dim3(256), 0, st, c, a, Q, O, j[0]);
     else hipLaunchKernelGGL((cache_attn_narrow_kernel<D, DT>), dim3(NARROW_WGS), dim3(256), 0, st, c, a, Q, O, j[1]);
     const int n_wide = wide ? WIDE_WGS : 0, n_narrow = narrow ? NARROW_WGS : 0;
     hipLaunchKernelGGL((cache_join_kernel<D, DT>), dim3(n_wide + n_narrow), dim3(256), 0, st, c, a, n_narrow, O, j[0], j[1]);
