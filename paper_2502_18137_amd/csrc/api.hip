@@ -141,6 +141,19 @@ int check_token_strides(int64_t n, int64_t h) {
     return SPARGE_OK;
 }
 
+// Whether two of n x H rows of d elements share an element (strides >= d where there are two).
+bool rows_overlap(int64_t n, int64_t H, int64_t stride_n, int64_t stride_h, int64_t d) {
+    if (n < 2 || H < 2) return false;
+    typedef __int128 wide;
+    if (stride_n >= static_cast<wide>(H - 1) * stride_h + d || stride_h >= static_cast<wide>(n - 1) * stride_n + d) return false;
+    for (int64_t h = 1; h < H; ++h) {   // neither lies inside the other: the token rows next to the first token's row of head h
+        const wide at = static_cast<wide>(h) * stride_h, before = at / stride_n;
+        if (before < n && at - before * stride_n < d) return true;
+        if (before + 1 < n && (before + 1) * stride_n - at < d) return true;
+    }
+    return false;
+}
+
 // Partition of the scratch buffer.  Every entry point uses a subset; offsets are fixed by shape.
 struct Workspace {
     size_t pooled_q, ksum_t, sim_q, sim_k, k_mean, logits, Qq, Kq, q_scale, k_scale, v_tiles, mask, queue, total;
@@ -1011,7 +1024,8 @@ int sparge_cache_attn(const sparge_cache* cache, const void* Q, int n_slots, int
     if (misaligned(Q) || misaligned(O)) return fail(SPARGE_EINVAL, "tensor pointers must be 16-byte aligned");
     if (off4(cu)) return fail(SPARGE_EINVAL, "cu must be 4-byte aligned");
     if ((rc = check_token_strides(q_stride_n, q_stride_h)) || (rc = check_token_strides(o_stride_n, o_stride_h))) return rc;
-    if ((n_slots > 1 && o_stride_n < cache->d) || (H > 1 && o_stride_h < cache->d)) return fail(SPARGE_EINVAL, "rows of O must not overlap");
+    if ((n_slots > 1 && o_stride_n < cache->d) || (H > 1 && o_stride_h < cache->d) || rows_overlap(n_slots, H, o_stride_n, o_stride_h, cache->d))
+        return fail(SPARGE_EINVAL, "rows of O must not overlap");
     if (!(sm_scale < INFINITY)) return fail(SPARGE_EINVAL, "sm_scale must be finite");
     const size_t need = cache_attn_workspace(cache->d);
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256) return fail(SPARGE_EINVAL, "workspace must be 256-byte aligned device memory");
