@@ -339,8 +339,8 @@ int sparge_cache_plan(const sparge_cache* cache, const int32_t* new_len, const u
                       int32_t* slots, int32_t* req, int32_t* status, void* hip_stream);
 
 /*
- * Stores the step's new tokens: K, V 16-bit [n_slots, H_kv, d] (element strides per token and head, multiples of 8; d
- * contiguous; 16-byte aligned), token i to slots[i] of row req[i], as sparge_cache_plan gave them.  Every page that gets
+ * Stores the step's new tokens: K, V 16-bit [n_slots, H_kv, d] (element strides per token and head, multiples of 8, of one
+ * token or one head any; d contiguous; 16-byte aligned), token i to slots[i] of row req[i], as sparge_cache_plan gave them.  Every page that gets
  * a token is quantized anew from all its tokens.  Tokens with slot -1 are skipped.  The same call may be repeated as long as
  * the step's tokens did not open another page of a row whose last page was partly filled.
  */

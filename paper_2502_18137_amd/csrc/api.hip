@@ -135,7 +135,10 @@ int check_slots(int n) {
     return SPARGE_OK;
 }
 
-int check_token_strides(int64_t n, int64_t h) {
+// of [n_slots, heads, d] tokens; the stride of a dimension of size 1 may be anything and becomes 0
+int check_token_strides(int n_slots, int heads, int64_t& n, int64_t& h) {
+    if (n_slots == 1) n = 0;
+    if (heads == 1) h = 0;
     if (n < 0 || h < 0) return fail(SPARGE_EINVAL, "bad strides");
     if (n % 8 || h % 8) return fail(SPARGE_EINVAL, "strides must be multiples of 8 elements");
     return SPARGE_OK;
@@ -982,7 +985,8 @@ int sparge_cache_append(const sparge_cache* cache, const void* K, const void* V,
     if (!K || !V || !cu || !slots || !req) return fail(SPARGE_EINVAL, "NULL argument");
     if (misaligned(K) || misaligned(V)) return fail(SPARGE_EINVAL, "tensor pointers must be 16-byte aligned");
     if (off4(cu) || off4(slots) || off4(req)) return fail(SPARGE_EINVAL, "int32 arrays must be 4-byte aligned");
-    if ((rc = check_token_strides(k_stride_n, k_stride_h)) || (rc = check_token_strides(v_stride_n, v_stride_h))) return rc;
+    if ((rc = check_token_strides(n_slots, cache->H_kv, k_stride_n, k_stride_h)) || (rc = check_token_strides(n_slots, cache->H_kv, v_stride_n, v_stride_h)))
+        return rc;
     hipError_t e = launch_cache_append(*cache, K, V, n_slots, k_stride_n, k_stride_h, v_stride_n, v_stride_h, cu, slots, req,
                                        static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? SPARGE_OK : hip_fail(e, "cache_append");
@@ -1023,7 +1027,7 @@ int sparge_cache_attn(const sparge_cache* cache, const void* Q, int n_slots, int
     if (!Q || !O || !cu) return fail(SPARGE_EINVAL, "NULL argument");
     if (misaligned(Q) || misaligned(O)) return fail(SPARGE_EINVAL, "tensor pointers must be 16-byte aligned");
     if (off4(cu)) return fail(SPARGE_EINVAL, "cu must be 4-byte aligned");
-    if ((rc = check_token_strides(q_stride_n, q_stride_h)) || (rc = check_token_strides(o_stride_n, o_stride_h))) return rc;
+    if ((rc = check_token_strides(n_slots, H, q_stride_n, q_stride_h)) || (rc = check_token_strides(n_slots, H, o_stride_n, o_stride_h))) return rc;
     if ((n_slots > 1 && o_stride_n < cache->d) || (H > 1 && o_stride_h < cache->d) || rows_overlap(n_slots, H, o_stride_n, o_stride_h, cache->d))
         return fail(SPARGE_EINVAL, "rows of O must not overlap");
     if (!(sm_scale < INFINITY)) return fail(SPARGE_EINVAL, "sm_scale must be finite");

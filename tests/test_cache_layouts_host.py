@@ -34,3 +34,15 @@ def test_results_that_share_elements(lib):  # noqa: F811
 @pytest.mark.parametrize("n,H,s,o,want", [(1, 4, (256, 64), (0, 64), NO_SPACE), (3, 1, (64, 64), (64, 0), NO_SPACE), (1, 1, (64, 64), (0, 0), NO_SPACE)])
 def test_lone_rows_share_nothing(lib, n, H, s, o, want):  # noqa: F811
     assert call(lib, n, H, s, o, H_kv=1) == want
+
+
+@pytest.mark.parametrize("n,H,s,o", [(1, 4, (333, 64), (7, 64)), (1, 4, (-8, 64), (-1, 64)), (3, 1, (64, 5), (64, 9)), (1, 1, (3, 3), (5, -5))])
+def test_strides_that_say_nothing(lib, n, H, s, o):  # noqa: F811
+    """of a dimension of size 1: any number"""
+    assert call(lib, n, H, s, o, H_kv=1) == NO_SPACE
+
+
+@pytest.mark.parametrize("n,H,s,o", [(2, 4, (333, 64), (256, 64)), (3, 2, (128, 60), (128, 64)), (3, 1, (60, 64), (64, 64)), (1, 2, (64, -8), (64, 64)),
+                                     (3, 1, (64, 64), (8, 64)), (1, 2, (64, 64), (64, 56))])
+def test_strides_that_count(lib, n, H, s, o):  # noqa: F811
+    assert call(lib, n, H, s, o, H_kv=1) == BAD
