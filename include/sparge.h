@@ -352,7 +352,7 @@ int sparge_cache_append(const sparge_cache* cache, const void* K, const void* V,
  * Reads tokens back as the values that their codes stand for (with k_shift added again): K, V [n_slots, H_kv, d]
  * contiguous, 16-byte aligned, SPARGE_F32 (code amax / 127 + shift rounded once) or the cache's dtype (that, rounded to it).
  * slots: any, in any order (64 table[r, t / 64] + t % 64 for token t of row r); outputs of slots outside the pool stay as
- * they were.  req: the rows, for k_shift (NULL allowed without).
+ * they were.  req: the rows, for k_shift (without it not looked at, NULL allowed; with it outputs of other rows stay, too).
  */
 int sparge_cache_read(const sparge_cache* cache, const int32_t* slots, const int32_t* req, int n_slots, int out_dtype, void* K,
                       void* V, void* hip_stream);

@@ -674,6 +674,7 @@ hipError_t launch_cache_append(const sparge_cache& c, const void* K, const void*
 
 hipError_t launch_cache_read(const sparge_cache& c, const int32_t* slots, const int32_t* req, int n_slots, int out_dtype, void* K,
                              void* V, hipStream_t st) {
+    if (!c.k_shift) req = nullptr;   // the rows are asked for the shift alone
     const int window = window_of(n_slots, c.H_kv, 512);
     const dim3 grid((n_slots + window - 1) / window, c.H_kv, 2);
 #define READ(D, OUT) hipLaunchKernelGGL((cache_read_kernel<D, OUT>), grid, dim3(256), 0, st, c, slots, req, n_slots, window, K, V)

@@ -27,3 +27,24 @@ def test_one_token_or_one_head_with_any_stride(sp, n, heads):
         assert got[-1][2] is out
     for a, b in zip(*got):
         assert torch.equal(a, b) and bool(torch.isfinite(a.float()).all())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_rows_that_nobody_needs_are_not_looked_at(sp, dtype):
+    """without a shift a read depends on its slots alone, whatever rows come with them; with one, a row outside the cache has no value"""
+    import torch
+    dt = getattr(torch, dtype)
+    x = torch.randn(100, 2, 64, device="cuda").bfloat16()
+    for shift in (None, torch.randn(2, 2, 64, device="cuda")):
+        c = sp.SpargeCache(2, 2, 64, 6, 3, k_shift=shift)
+        plan = sp.sparge_cache_plan(c, torch.tensor([30, 70], dtype=torch.int32, device="cuda"), 100)
+        sp.sparge_cache_append(c, x, x, plan)
+        want = sp.sparge_cache_read(c, plan.slots, plan.req, dtype=dt)
+        for wrong in (-1, 2, 2 ** 31 - 1):
+            req = plan.req.clone()
+            req[20:50] = wrong
+            out = tuple(torch.full_like(w, 7.0) for w in want)
+            got = sp.sparge_cache_read(c, plan.slots, req, dtype=dt, out=out)
+            for a, b in zip(got, want):
+                assert torch.equal(a[:20], b[:20]) and torch.equal(a[50:], b[50:])
+                assert torch.equal(a[20:50], b[20:50]) if shift is None else bool((a[20:50] == 7).all())
