@@ -64,10 +64,10 @@ struct CacheAttn {
 struct JoinDesc {
     int n_parts;                        // that the item has; 0: nothing to join here
     int first, part;                    // the first part that begins inside the item; this one
-    int token, n_tok, head, n_heads;    // the item's rows of Q and O
-    int pad;                            // (two 16-byte loads)
+    int token, n_tok, head;             // the item's rows of Q and O: tokens, their first head
+    int pad[2];                         // (two 16-byte loads)
 };
-constexpr JoinDesc NO_JOIN = {0, 0, 0, 0, 0, 0, 0, 0};
+constexpr JoinDesc NO_JOIN = {0, 0, 0, 0, 0, 0, {0, 0}};
 size_t cache_attn_workspace(int d);
 
 hipError_t launch_cache_plan(const sparge_cache& c, const int32_t* new_len, const uint8_t* release, int n_slots, int32_t* cu,

@@ -88,15 +88,13 @@ __device__ __forceinline__ v8h codes8(uint32_t a, uint32_t b) {
     return r;
 }
 
-// How a row's query rows are cut into tiles of up to `rows`: TT whole tokens of Gp heads, or, where a token's group exceeds a
-// tile, `parts` pieces of the group.
+// How a row's query rows are cut into tiles of up to `rows`: TT whole tokens of G heads.  (The narrow kernel gets groups of up to its
+// 16 rows, the wide one all there are.)
 struct Cut {
-    int G, Gp, parts, TT;
+    int G, TT;
 };
-__host__ __device__ inline Cut cut_of(int G, int rows) {
-    if (G <= rows) return {G, G, 1, rows / G};
-    return {G, rows, (G + rows - 1) / rows, 1};
-}
+static_assert(SPARGE_MAX_HEADS <= WIDE_ROWS, "a token's group fits a tile");
+__device__ __forceinline__ Cut cut_of(int G, int rows) { return {G, rows / G}; }
 
 // Which rows a line holds: those of more than `above` and at most `upto` query rows of a kv head.
 struct Rows {
@@ -177,9 +175,9 @@ struct Line {
     }
 };
 // A part that begins inside an item: what the join needs.  start, end: the item on the line; token, head: its first.
-__device__ __forceinline__ JoinDesc boundary(const Line& line, int part, u64 start, u64 end, int token, int n_tok, int head, int n_heads) {
+__device__ __forceinline__ JoinDesc boundary(const Line& line, int part, u64 start, u64 end, int token, int n_tok, int head) {
     const int first = line.part_of(start) + 1;                   // the first part that begins inside it
-    return {line.part_of(end - 1) - first + 2, first, part, token, n_tok, head, n_heads, 0};
+    return {line.part_of(end - 1) - first + 2, first, part, token, n_tok, head, {0, 0}};
 }
 
 // The blocks of an item's range, 64 table entries at a time, one a lane, the next 64 on their way.
@@ -389,7 +387,7 @@ struct NarrowShared {
 // The line of blocks.  (All tiles of a row count with all its blocks: they are few here.)
 struct NarrowLine {
     Cut cut;
-    int heads, per;                     // pieces of heads; rows per thread
+    int heads, per;                     // kv heads; rows per thread
     Line line;
     Rows which;                         // its rows
     bool others;                        // whether there are others
@@ -402,7 +400,7 @@ template <bool MIXED>
 __device__ __forceinline__ NarrowLine narrow_line(const sparge_cache& c, const CacheAttn& a, NarrowShared& sh) {
     NarrowLine x;
     x.cut = cut_of(a.H / c.H_kv, NARROW_ROWS);
-    x.heads = c.H_kv * x.cut.parts, x.per = (c.R + 255) / 256, x.which = ALL_ROWS, x.others = false;
+    x.heads = c.H_kv, x.per = (c.R + 255) / 256, x.which = ALL_ROWS, x.others = false;
     const int tid = threadIdx.x, r0 = tid * x.per, r1 = min(r0 + x.per, c.R);
     constexpr int N = MIXED ? 2 : 1;    // rows of one tile; of several
     u64 mine[N] = {}, total[N];
@@ -469,7 +467,7 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
 
     struct Item {
         RowInfo x;
-        int row, kh, gpart, tile, ntok, b0, b1, blocks;
+        int row, kh, tile, ntok, b0, b1, blocks;
     };
     auto next_item = [&](Item& it) -> bool {
         if (left == 0) return false;
@@ -486,7 +484,7 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
             }
         }
         it.x = info, it.row = r, it.tile = tile, it.blocks = row_blocks, it.b0 = b_next;
-        it.kh = head / cut.parts, it.gpart = head - it.kh * cut.parts;
+        it.kh = head;
         it.ntok = min(cut.TT, info.n - tile * cut.TT);
         const int take = static_cast<int>(min(static_cast<u64>(row_blocks - b_next), left));
         it.b1 = b_next += take;
@@ -500,8 +498,8 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
     int out_token = 0, out_head = 0;    // the lane's row of Q and O
     bool valid = false;
     auto open = [&](const Item& it) {
-        const int row = lane & 15, tok = row / cut.Gp, g = it.gpart * NARROW_ROWS + row - tok * cut.Gp;
-        valid = tok < it.ntok && g < cut.G;
+        const int row = lane & 15, tok = row / cut.G, g = row - tok * cut.G;
+        valid = tok < it.ntok;
         const int t = it.tile * cut.TT;
         limit = !valid ? -1 : a.causal ? min(it.x.p0 + t + tok, it.x.len - 1) : it.x.len - 1;
         lim_lo = a.causal ? min(it.x.p0 + t, it.x.len - 1) : it.x.len - 1;
@@ -527,10 +525,8 @@ __device__ __forceinline__ void narrow(const sparge_cache& c, const CacheAttn& a
     JoinDesc join = NO_JOIN;
     if (have) {
         open(it);
-        const int g0 = it.gpart * NARROW_ROWS;   // (worked out while the table is on its way)
-        if (it.b0 > 0)
-            join = boundary(line, part, lo - it.b0, lo - it.b0 + it.blocks, it.x.first + it.tile * cut.TT, it.ntok, it.kh * cut.G + g0,
-                            min(cut.Gp, cut.G - g0));
+        if (it.b0 > 0)   // (worked out while the table is on its way)
+            join = boundary(line, part, lo - it.b0, lo - it.b0 + it.blocks, it.x.first + it.tile * cut.TT, it.ntok, it.kh * cut.G);
         more = blocks.next(c, it.kh, block, page, at);
         if (more) {
             load_k(page, it.kh);
@@ -676,7 +672,7 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
     auto& lds_v = sh.v;
     const int tid = opaque(threadIdx.x), lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
     const Cut cut = cut_of(a.H / c.H_kv, WIDE_ROWS);
-    const int heads = c.H_kv * cut.parts;
+    const int heads = c.H_kv;
 
     // ---- this workgroup's part of the line, in keys
     const int per = (c.R + 255) / 256;
@@ -718,7 +714,7 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
     RowInfo x = uniform(sh.info);
     u64 left = line.begin(part + 1) - lo;                     // keys that this workgroup still has to take
     JoinDesc join = NO_JOIN;
-    // where it begins: head (with the group's part), tile, key
+    // where it begins: head, tile, key
     const u64 rem = uniform(sh.rem), chunk = max(length_of(x), static_cast<u64>(1));
     int head = static_cast<int>(quotient(rem, chunk)), i = 0;
     const u64 in = rem - head * chunk;
@@ -731,24 +727,24 @@ __device__ __forceinline__ void wide(const sparge_cache& c, const CacheAttn& a, 
 
     while (left > 0) {
         const int ntok = min(cut.TT, x.n - i * cut.TT), token0 = x.first + i * cut.TT;
-        const int kh = head / cut.parts, g0 = (head - kh * cut.parts) * WIDE_ROWS, n_heads = min(cut.Gp, cut.G - g0);
+        const int kh = head;
         const int vis = a.causal ? x.p0 + i * cut.TT + ntok : x.len;
         const int take = static_cast<int>(min(static_cast<u64>(vis - x0), left)), x1 = x0 + take;
         const int b0 = x0 / PAGE, b1 = x1 == vis ? (vis + PAGE - 1) / PAGE : x1 / PAGE;
         const bool whole = x0 == 0 && x1 == vis, is_first = left == line.begin(part + 1) - lo;
-        if (is_first && x0 > 0) join = boundary(line, part, lo - x0, lo - x0 + vis, token0, ntok, kh * cut.G + g0, n_heads);
+        if (is_first && x0 > 0) join = boundary(line, part, lo - x0, lo - x0 + vis, token0, ntok, kh * cut.G);
 
         // this wave's rows, the lane's one of them, and the least and the largest key that a row sees last
-        const int n_rows = ntok * cut.Gp, w0 = wave * 32, w1 = min(w0 + 32, n_rows) - 1;
-        const int row = w0 + (lane & 31), tok = row / cut.Gp, g = row - tok * cut.Gp;
-        const bool valid = row < n_rows && g < n_heads;
+        const int n_rows = ntok * cut.G, w0 = wave * 32, w1 = min(w0 + 32, n_rows) - 1;
+        const int row = w0 + (lane & 31), tok = row / cut.G, g = row - tok * cut.G;
+        const bool valid = row < n_rows;
         const int first_limit = a.causal ? x.p0 + i * cut.TT : x.len - 1;
         const int limit = !valid ? -1 : min(first_limit + (a.causal ? tok : 0), x.len - 1);
-        const int lim_lo = min(first_limit + (a.causal ? w0 / cut.Gp : 0), x.len - 1);
-        const int lim_hi = w1 < w0 ? -1 : min(first_limit + (a.causal ? w1 / cut.Gp : 0), x.len - 1);
+        const int lim_lo = min(first_limit + (a.causal ? w0 / cut.G : 0), x.len - 1);
+        const int lim_hi = w1 < w0 ? -1 : min(first_limit + (a.causal ? w1 / cut.G : 0), x.len - 1);
         Blocks blocks;
         blocks.open(c, a, r, kh, b0, min(b1, (x.len + PAGE - 1) / PAGE));
-        const long long token = token0 + tok, hd = kh * cut.G + g0 + g;
+        const long long token = token0 + tok, hd = kh * cut.G + g;
         uint4 q_raw[KS];
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
@@ -1003,13 +999,13 @@ __global__ __launch_bounds__(256, 2) void cache_attn_both_kernel(sparge_cache c,
 // PG groups of lanes every PG-th part, up to eight of them in one round trip to memory.  What is joined are means of the values, with
 // weights that add up to 1: no sum leaves fp32's range where the result does not.
 template <int D, int DT, int ROWS, int PG>
-__device__ __forceinline__ void join_item(const JoinDesc& d, int me, int workers, int Gp, const CacheAttn& a, uint16_t* O, const Joint& ws) {
+__device__ __forceinline__ void join_item(const JoinDesc& d, int me, int workers, int G, const CacheAttn& a, uint16_t* O, const Joint& ws) {
     constexpr int LANES = 64 / PG;
-    const int lane = threadIdx.x & 63, grp = lane / LANES, n_chunks = (d.n_tok * Gp * D * PG + 255) / 256;
+    const int lane = threadIdx.x & 63, grp = lane / LANES, n_chunks = (d.n_tok * G * D * PG + 255) / 256;
     for (int chunk = me; chunk < n_chunks; chunk += workers) {
         const int flat = chunk * (256 / PG) + (lane % LANES) * 4, row = flat / D, ch = flat % D;
-        const int tok = row / Gp, g = row - tok * Gp;
-        const bool there = tok < d.n_tok && g < d.n_heads;
+        const int tok = row / G, g = row - tok * G;
+        const bool there = tok < d.n_tok;
         float m = FAR, l = 0.f;
         v4f o = {0.f, 0.f, 0.f, 0.f};
         for (int k0 = grp; k0 < d.n_parts; k0 += 8 * PG) {
@@ -1063,11 +1059,11 @@ __device__ __forceinline__ void join(const sparge_cache& c, const CacheAttn& a, 
     const int wave = uniform(static_cast<int>(threadIdx.x) >> 6);
     const JoinDesc d = ws.desc[(bid * 4 + wave) / WAVES];
     if (d.n_parts == 0) return;
-    const int Gp = cut_of(a.H / c.H_kv, ROWS).Gp, me = (d.part - d.first) * WAVES + wave % WAVES, workers = (d.n_parts - 1) * WAVES;
+    const int G = a.H / c.H_kv, me = (d.part - d.first) * WAVES + wave % WAVES, workers = (d.n_parts - 1) * WAVES;
     // as many groups of lanes as bring an item's parts in with one round trip, while its waves have chunks enough
-    if (d.n_parts <= 4) join_item<D, DT, ROWS, 1>(d, me, workers, Gp, a, O, ws);
-    else if (d.n_parts <= 64) join_item<D, DT, ROWS, 8>(d, me, workers, Gp, a, O, ws);
-    else join_item<D, DT, ROWS, 32>(d, me, workers, Gp, a, O, ws);
+    if (d.n_parts <= 4) join_item<D, DT, ROWS, 1>(d, me, workers, G, a, O, ws);
+    else if (d.n_parts <= 64) join_item<D, DT, ROWS, 8>(d, me, workers, G, a, O, ws);
+    else join_item<D, DT, ROWS, 32>(d, me, workers, G, a, O, ws);
 }
 // the first n_narrow workgroups take the narrow kernel's parts, the others the wide one's
 template <int D, int DT>
