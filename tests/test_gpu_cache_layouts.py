@@ -48,3 +48,24 @@ def test_rows_that_nobody_needs_are_not_looked_at(sp, dtype):
             for a, b in zip(got, want):
                 assert torch.equal(a[:20], b[:20]) and torch.equal(a[50:], b[50:])
                 assert torch.equal(a[20:50], b[20:50]) if shift is None else bool((a[20:50] == 7).all())
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_tokens_and_queries_that_share_memory(sp, new):
+    """inputs of stride 0: one head's queries for all heads, one token's K, V and queries for all tokens"""
+    import torch
+    d, dt = 64, torch.float16
+    g = torch.Generator(device="cuda").manual_seed(new)
+    x = torch.randn(3, 1, 1, d, generator=g, device="cuda").to(dt)
+    K, V, Q = x[0].expand(2 * new, 2, d), x[1].expand(2 * new, 2, d), x[2].expand(2 * new, 8, d)
+    got = []
+    for whole in (False, True):
+        c = sp.SpargeCache(2, 2, d, 8, 4, dtype=dt)
+        plan = sp.sparge_cache_plan(c, torch.tensor([new, new], dtype=torch.int32, device="cuda"), 2 * new)
+        k, v, q = (t.contiguous() if whole else t for t in (K, V, Q))
+        sp.sparge_cache_append(c, k, v, plan)
+        got.append(sp.sparge_cache_attn(c, q, plan, out=torch.zeros(2 * new, 8, d, dtype=dt, device="cuda")))
+    assert torch.equal(*got)
+    # the same value everywhere: any weights give it back, within its rounding to a code (amax / 254) and that of the result
+    v = x[1].float()
+    assert bool(((got[0].float() - v).abs() <= v.abs().max() / 254 + v.abs() * 2.0 ** -10).all())

@@ -90,3 +90,56 @@ def test_fp16_rows_do_not_lose_bits_to_their_neighbours(sp, G, few, many):
             error, rounding = error + np.square(got[at:at + n] - want).sum(), rounding + np.square(m.round16(want) - want).sum()
         at += n
     assert error <= 1.05 ** 2 * rounding, (error / rounding) ** 0.5
+
+
+def test_a_captured_step_whose_rows_change(sp):
+    """one graph of plan, append and attention, replayed with other rows adding other numbers of tokens every time: single tokens, rows of
+    several tiles in little work, a long piece beside them, nothing at all; equal to the oracle, and to the call itself, bit by bit"""
+    import torch
+    m = Model(sp, 6, 2, 64, 400, 110, dtype="bf16", seed=130)
+    m.step([6000, 3, 127, 200, 0, 64])
+    slots = 400
+    x = [torch.zeros(slots, h, 64, dtype=m.dt, device="cuda") for h in (2, 2, 8)]
+    new = m.i32([0] * 6)
+    plan = sp.CachePlan(*[torch.zeros(n, dtype=torch.int32, device="cuda") for n in (7, slots, slots, 2)])
+    ws = torch.empty(sp.sparge_cache_attn_workspace_bytes(m.cache, 8), dtype=torch.uint8, device="cuda")
+    out = torch.zeros(slots, 8, 64, dtype=m.dt, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        sp.sparge_cache_plan(m.cache, new, slots, out=plan)
+        sp.sparge_cache_append(m.cache, x[0], x[1], plan)
+        sp.sparge_cache_attn(m.cache, x[2], plan, ws=ws, out=out)
+    for step in ([1] * 6, [300, 1, 1, 1, 1, 1], [0, 40, 0, 7, 1, 0], [0] * 6, [2, 0, 5, 0, 350, 1], [1, 1, 0, 1, 1, 1]):
+        n = sum(step)
+        (K, V), m.new = m.tokens(n), step
+        q = m.queries(8)
+        for t, v in zip(x, (K, V, q)):
+            t[:n].copy_(m.gpu(v))
+        new.copy_(m.i32(step))
+        out.fill_(7.25)
+        m.book.plan(step, None, slots)
+        at = 0
+        for r, k in enumerate(step):
+            m.K[r], m.V[r] = np.concatenate([m.K[r], K[at:at + k]]), np.concatenate([m.V[r], V[at:at + k]])
+            at += k
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert plan.status[0] == 0 and m.cache.length.tolist() == m.book.length
+        m.check_stored()
+        eager, _ = m.check_attn(plan, 8, q=q, pad=slots - n)
+        assert np.array_equal(out.double().cpu().numpy(), eager)
+
+
+@pytest.mark.parametrize("G", [1, 4, 20])
+def test_pieces_among_all_rows_there_can_be(sp, G):
+    """4096 rows, several to a thread that looks for them; two of them add long pieces, some a token or a few"""
+    m = Model(sp, 4096, 2, 64, 4500, 110, dtype="fp16", seed=140 + G)
+    held = m.rng.integers(0, 4, 4096)
+    held[[777, 4095]] = 5000, 1500
+    m.step(held.tolist())
+    new = (m.rng.random(4096) < 0.02).astype(int)
+    new[[3, 776, 2000]] = 9, 2, 30
+    new[[777, 4095]] = 300, 260
+    m.check_attn(m.step(new.tolist(), pad=2), 2 * G, pad=2)
