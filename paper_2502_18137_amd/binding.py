@@ -578,7 +578,8 @@ def sparge_cache_append(cache: SpargeCache, K: torch.Tensor, V: torch.Tensor, pl
 def sparge_cache_read(cache: SpargeCache, slots: torch.Tensor, req: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
                       out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """-> K, V [n, H_kv, d]: the values that the codes of these slots (int32 [n]) stand for, in fp32 or the cache's dtype (default).
-    req: the slots' rows, int32 [n], for a cache with k_shift.  Outputs of slots outside the pool are left as they were."""
+    req: the slots' rows, int32 [n], for a cache with k_shift (not looked at without).  Outputs of slots outside the pool are left as
+    they were: without `out` that is whatever the new tensors' memory held."""
     dtype = dtype or cache.dtype
     if dtype is not torch.float32 and dtype is not cache.dtype:
         raise SpargeError(f"dtype {dtype} is neither fp32 nor the cache's {cache.dtype}")
@@ -610,7 +611,9 @@ def sparge_cache_attn(cache: SpargeCache, Q: torch.Tensor, plan: CachePlan, caus
                       mask: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the step's tokens, Q [n_slots, H, d], over the cache (after sparge_cache_append).  mask: uint8
-    [R, H_kv, max_blocks], 0 = no key of that block is seen.  -> O like Q (rows that are no token of the step: as they were)."""
+    [R, H_kv, max_blocks], 0 = no key of that block is seen.  -> O like Q.  Rows that are no token of the step, which is all of them if
+    the plan did not fit, are left as they were: without `out` that is whatever the new tensor's memory held.  ws: a uint8 tensor of
+    sparge_cache_attn_workspace_bytes (52 or 102 MB for d = 64 or 128, whatever the step) that a program of many calls keeps."""
     _same_rows(cache, plan)
     n = plan.n_slots
     if Q.dim() != 3:

@@ -85,7 +85,8 @@ __device__ __forceinline__ void fill_slot(const sparge_cache& c, const int* cu, 
 // What bounds it is a chain of four round trips to memory (lengths; the pages that rows give up; the pages that rows take;
 // the table entries that slots are made of), so rows, pages and slots are spread over the threads through the prefix sums,
 // and the instructions that it runs once: loops that are short anyway stay rolled up (unrolled, with the rows kept in
-// registers, 11 us in the place of 6 for 48 rows; it is 4.7 us now, and 16 for 1000 rows of which 200 give up 9000 pages).
+// registers, 11 us in the place of 6 for 48 rows; it is 4.7 us now, and 16 for 1000 rows of which 200 give up 9200 pages and
+// 410 are taken; 15 where 1000 rows take 10000, 22 where they give up as many, too).
 __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c, const int32_t* __restrict__ new_len,
                                                                   const uint8_t* __restrict__ release, int n_slots, int32_t* cu,
                                                                   int32_t* slots, int32_t* req, int32_t* status) {
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void cache_plan_kernel(sparge_cache c
 #pragma unroll 1
     for (int pop = 0; pop < 2; ++pop) {
         // Pages are dealt out eight a thread, in the rows' order: every row writes its number where its pages begin, and the
-        // largest number up to a place is the place's row.  (One compute unit's issue is what bounds this: for the 9000 pages that 200
+        // largest number up to a place is the place's row.  (The one workgroup's issue is what bounds this: for the 9000 pages that 200
         // of 1000 rows give up, the kernel takes 25 us with a search per page through the prefix sums, 21 to 23 with pieces of
         // rows dealt to waves, 16 like this.)
         const int* prefix = pop ? need_at : push_at;
@@ -312,9 +313,10 @@ __device__ __forceinline__ void heads_first(int window, int& hk, int& i0) {
 // A workgroup quantizes one kv head's K or V of every page that begins to get tokens inside its window of `window` (a power of two
 // up to 64) slots: the open page's older tokens from the tail, the new ones from the call's tensor.  Bound by its bytes: a
 // thread holds what makes whole 16-byte pieces of the page (K: 16 channels of a token; V: a channel of 16 tokens), loads and
-// stores are coalesced and nothing goes through LDS but the maxima: 65k tokens of 16 heads of 128 channels, 805 MB, in 190 us, 4.2 TB/s,
-// where a large copy reaches 5.  (K and V of a page in one workgroup, their loads together: 69 us in the place of 57 for
-// 29k tokens of 8 heads.)  Where a page gets few tokens that do not raise its amax
+// stores are coalesced and nothing goes through LDS but the maxima: 65k tokens of 16 heads of 128 channels, 805 MB that no cache holds,
+// in 151 us, 5.3 TB/s, with a shift 155, where a large copy reaches 5; 29k tokens of 8 heads 39 and 42 us.  Behind a
+// read-back to fp32, whose stores are 1.07 and 0.24 GB, these take 190 and 57 us.  (K and V of a page in one workgroup, their loads
+// together: 69 us in the place of those 57.)  Where a page gets few tokens that do not raise its amax
 // (decoding: all but one of t + 1 at the t-th token of a page), the older codes are what they were and only the new ones are
 // written; the tail's amax per token tells without reading the tail.
 // The row's first page also stores the tokens of the row's last page if that stays open (after it has read the older

@@ -643,10 +643,11 @@ __device__ __forceinline__ float convert_q32(const uint4 (&raw)[D / 16], v8h (&q
     }
 }
 
-// Bound by the issue of vector instructions (the conversions, the exponentials) beside the products, at the clock that the power limit leaves: of a
-// compute unit's cycles the vector ALU issues in 61 %, the matrix pipe works in 42 %, LDS moves data in two thirds.  3 rows of 700 to 2048 tokens
-// over 4000 to 30000 keys, 32 heads over 8: 540 GFLOP in 650 us with the join, 0.83 PFLOP/s, where a large bf16 product reaches
-// 1.14.  (64 query rows a wave, one workgroup a compute unit: 1147 us in the place of 917.)
+// No unit is full, at the clock that the power limit leaves: of a compute unit's cycles the vector ALU issues in 62 % (conversions,
+// exponentials), the matrix pipe works in 43 %, LDS in 38 %, a seventh of that for bank conflicts; of their own cycles the two waves a
+// SIMD issue in 48 %, wait to issue in 29 % and for memory, LDS or the others in 23 %.  3 rows of 700 to 2048 tokens over 4000 to 30000
+// keys, 32 heads over 8: 540 GFLOP in 640 us with the join, 0.84 PFLOP/s, where a large bf16 product reaches 1.14.  (64 query rows a wave,
+// one workgroup a compute unit, before the loop's order was laid down: 1147 us in the place of 917.)
 // Four waves share the blocks: their codes are converted once per workgroup into LDS, in the operand order of the 32x32x16 MFMA
 // (two buffers, one barrier a block; the raw bytes of the block after the next are on their way meanwhile), and every wave
 // reads them for its own 32 query rows.  In that MFMA's accumulators a lane owns one query (lane % 32) and, of every 16 keys,
