@@ -1118,8 +1118,8 @@ hipError_t launch_cache_attn(const sparge_cache& c, const CacheAttn& a, const vo
     // 26 us, wide 36; 16 queries: 30 and 38).  The narrow kernel alone runs where no row can have more than a tile; a single row's
     // tokens are the wide kernel's from half a tile on (9000 keys, 4 queries a head: 2 tokens narrow 17.8 us, wide 18.1; 4 tokens 22.3
     // and 18.6; 8 tokens 27.2 and 18.9).  Else one kernel holds both, which costs a step of single tokens 0.1 to 0.9 us, and shares
-    // the rows out on the device (255 rows of one token beside one of 1500 over 30000 keys, 1 query a head: 554 us, the narrow kernel
-    // alone 1124; one row of 500 tokens over 9000 keys among 511 idle ones: 144 and 276).
+    // the rows out on the device (255 rows of one token beside one of 1500 over 30000 keys, 1 query a head: 549 us, the narrow kernel
+    // alone 1059; one row of 500 tokens over 9000 keys among 511 idle ones: 141 and 267).
     const long long G = a.H / c.H_kv, most = a.n_slots * G;
     const bool few = c.R > 1 ? most <= NARROW_ROWS : a.n_slots == 1 || most <= NARROW_ROWS / 2;
     const bool narrow = G <= NARROW_ROWS && (few || c.R > 1), wide = G > NARROW_ROWS || !few;
