@@ -368,8 +368,8 @@ int sparge_cache_read(const sparge_cache* cache, const int32_t* slots, const int
  * power of two per row, in fp16), the weights times V's scale rounded to fp16 (fp16 tokens, rows of up to 64 query rows of a kv
  * head: in two parts, to 22 bits) beside the query's own largest weight times scale, of which they keep what is 2^-34 or
  * more; weights below 2^-126 of a query's largest may count as 0.  The result does not depend on timing.
- * O must not overlap Q, nor its rows each other (refused).  The workspace (256-byte aligned) carries nothing between calls; calls
- * that may overlap need one each.
+ * O must not overlap Q (O = Q is refused), nor its rows each other (refused).  The workspace (256-byte aligned) carries nothing
+ * between calls; calls that may overlap need one each.
  */
 int sparge_cache_attn_workspace_bytes(const sparge_cache* cache, int H, size_t* bytes /* host, out */);
 int sparge_cache_attn(const sparge_cache* cache, const void* Q, int n_slots, int H, int64_t q_stride_n, int64_t q_stride_h,

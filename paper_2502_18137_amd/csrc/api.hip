@@ -1034,6 +1034,7 @@ int sparge_cache_attn(const sparge_cache* cache, const void* Q, int n_slots, int
     const size_t need = cache_attn_workspace(cache->d);
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256) return fail(SPARGE_EINVAL, "workspace must be 256-byte aligned device memory");
     if (ws_bytes < need) return fail(SPARGE_ENOSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
+    if (Q == O) return fail(SPARGE_EINVAL, "O must not overlap Q");
     CacheAttn a;
     a.n_slots = n_slots, a.H = H, a.causal = causal != 0;
     a.q_sn = q_stride_n, a.q_sh = q_stride_h, a.o_sn = o_stride_n, a.o_sh = o_stride_h;

@@ -46,3 +46,9 @@ def test_strides_that_say_nothing(lib, n, H, s, o):  # noqa: F811
                                      (3, 1, (64, 64), (8, 64)), (1, 2, (64, 64), (64, 56))])
 def test_strides_that_count(lib, n, H, s, o):  # noqa: F811
     assert call(lib, n, H, s, o, H_kv=1) == BAD
+
+
+def test_results_in_the_queries_place(lib):  # noqa: F811
+    """several workgroups read a token's queries, and one writes its results"""
+    rc = attn(lib, Q=8192, O=8192)
+    assert rc == BAD and b"overlap" in lib.sparge_last_error(), rc
